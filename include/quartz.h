@@ -49,9 +49,9 @@ typedef enum quartz_status {
     QUARTZ_ERR_NULL = 1,        /* a required pointer is NULL */
     QUARTZ_ERR_SHAPE = 2,       /* negative size, K % 64 != 0, ld too small, too large */
     QUARTZ_ERR_UNSUPPORTED = 3, /* group_size, lzs_group, mode or epilogue not supported */
-    QUARTZ_ERR_ALIGN = 4,       /* a pointer is not 16-byte aligned */
+    QUARTZ_ERR_ALIGN = 4,       /* a pointer or stride is not aligned (pointers: 16 bytes) */
     QUARTZ_ERR_HIP = 5,         /* the kernel launch failed */
-    QUARTZ_ERR_WORKSPACE = 6    /* workspace smaller than the size query asks for */
+    QUARTZ_ERR_WORKSPACE = 6    /* workspace missing or smaller than the size query asks for */
 } quartz_status;
 
 enum { QUARTZ_MODE_SYMMETRIC = 0, QUARTZ_MODE_ASYMMETRIC = 1 };
@@ -539,6 +539,161 @@ quartz_status quartz_w4a4_layer_kernel(int64_t M, int64_t N, int64_t K, int32_t 
 int64_t quartz_w4a4_linear_schedule(int64_t M, int64_t N, int64_t K, int32_t blocks,
                                     int32_t split, int32_t tiles, int32_t* schedule,
                                     int32_t* segments, int64_t capacity);
+
+/*
+ * ---------------------------------------------------------------- decoding
+ * A transformer's decoding step on 4-bit operands: MXFP4 linear layers, rotary
+ * positions, and attention of one new token over a paged cache.  Here int32
+ * arrays need 4-byte and the frequencies 8-byte alignment, not 16.
+ *
+ * MXFP4 (microscaled 4-bit floating point).  A block is 32 consecutive elements
+ * of a row.  With a = max|x| over the block, its scale is 2^E, E =
+ * max(floor(log2 a) - 2, -127) (-127 where a = 0), kept as the byte E + 127,
+ * and its elements are x 2^-E rounded to e2m1 (0, 0.5, 1, 1.5, 2, 3, 4, 6 and
+ * their negatives; nearest, ties to the even code, saturating at 6), 4 bits
+ * each: bit 3 the sign, bits 0..2 the index into that list.  A block that holds
+ * an infinity or a NaN has the byte 255: it stands for NaN, whatever its codes.
+ * Layout of an [R][K] tensor (activations: R = M, weights: R = N), K % 64 == 0:
+ *   codes   u8 [K/32][R][16]         byte i of (block, row): element 2i in the
+ *                                    low half, 2i + 1 in the high half
+ *   scales  u8 [ceil(K/128)][R][4]   byte j of (word w, row): block 4w + j (the
+ *                                    bytes past block K/32 - 1 are not read)
+ *
+ * quartz_mxfp4_quantize: x bf16 [M][ldx] -> codes and scales (activations, and
+ *   weights once per layer).  K <= ldx <= 2^24, ldx % 8 == 0.
+ * quartz_mxfp4_dequantize: the values they stand for, y bf16 [M][ldy] (exact;
+ *   beyond bf16's range infinite), ldy as ldx.
+ * quartz_mxfp4_linear: y[m][n] = bf16(act(sum over k of a[m][k] w[n][k] + bias[n])),
+ *   a and w the values of two MXFP4 tensors, products exact, sums in fp32.
+ *   bias bf16 [N] or NULL; y bf16 [M][ldy], N <= ldy <= 2^24; epilogue
+ *   QUARTZ_EPI_NONE or QUARTZ_EPI_GELU_TANH.  M = 0 or N = 0: nothing is done.
+ * quartz_mxfp4_linear_bf16: the same from bf16 activations x [M][ldx], which are
+ *   quantized as by quartz_mxfp4_quantize: within the kernel for few tokens
+ *   (quartz_mxfp4_linear_workspace_bytes is 0: no workspace), else into the
+ *   workspace (that many bytes, 16-byte aligned, any contents).
+ *   QUARTZ_ERR_WORKSPACE if it is missing or smaller.  Calls that share a
+ *   workspace must not overlap in time.
+ */
+quartz_status quartz_mxfp4_quantize(const void* x_bf16, int64_t M, int64_t K, int64_t ldx,
+                                    uint8_t* codes, uint8_t* scales, hipStream_t stream);
+
+quartz_status quartz_mxfp4_dequantize(const uint8_t* codes, const uint8_t* scales, int64_t M,
+                                      int64_t K, void* y_bf16, int64_t ldy, hipStream_t stream);
+
+quartz_status quartz_mxfp4_linear(const uint8_t* a_codes, const uint8_t* a_scales,
+                                  const uint8_t* w_codes, const uint8_t* w_scales,
+                                  const void* bias_bf16, void* y_bf16, int64_t M, int64_t N,
+                                  int64_t K, int64_t ldy, int32_t epilogue, hipStream_t stream);
+
+size_t quartz_mxfp4_linear_workspace_bytes(int64_t M, int64_t K);
+
+quartz_status quartz_mxfp4_linear_bf16(const void* x_bf16, int64_t ldx, const uint8_t* w_codes,
+                                       const uint8_t* w_scales, const void* bias_bf16, void* y_bf16,
+                                       int64_t M, int64_t N, int64_t K, int64_t ldy,
+                                       int32_t epilogue, void* workspace, size_t workspace_bytes,
+                                       hipStream_t stream);
+
+/*
+ * Rotary positions: pair i < rot / 2 of a head at position p is turned by p f_i
+ * turns, (a, b) -> magnitude (a cos - b sin, b cos + a sin); channels from rot
+ * on are copied.  QUARTZ_ROTARY_HALF pairs channels i and i + rot / 2,
+ * QUARTZ_ROTARY_INTERLEAVED 2i and 2i + 1.  inverse != 0 turns back, with the
+ * same magnitude: the transposed map, which takes the gradient of the output to
+ * that of the input.
+ *   x, y       bf16 [tokens][heads][d], unit stride along d, the other strides in
+ *              elements (any); y == x with equal strides works in place, other
+ *              overlaps do not.  Vectors are used where d % 16 == rot % 16 == 0
+ *              and pointers and strides are multiples of 16 bytes.
+ *   d, rot     even, 0 <= rot <= d.
+ *   positions  int32 [tokens], any value.
+ *   freqs      int64 [rot / 2]: f_i in units of 2^-64 turns, so that p f_i modulo
+ *              one turn is the 64-bit product (exact for every position).
+ *
+ * quartz_rotary_frequencies (host only, needs no GPU): freqs (HOST memory) of
+ * f_i = base^(-2i / rot) / (2 pi), for longer contexts scaled by `factor` >= 1:
+ *   QUARTZ_ROTARY_LINEAR  f_i / factor (factor 1: unscaled)
+ *   QUARTZ_ROTARY_BASE    base factor^(rot / (rot - 2)) in place of base
+ *   QUARTZ_ROTARY_PARTS   f_i (g + (1 - g) / factor), g = (original f_i - low) /
+ *                         (high - low) clamped to [0, 1]: pairs that turn often
+ *                         over the original context stay, slow ones are
+ *                         stretched.  low < high and original > 0 are read in
+ *                         this mode only.
+ */
+enum { QUARTZ_ROTARY_HALF = 0, QUARTZ_ROTARY_INTERLEAVED = 1 };
+enum { QUARTZ_ROTARY_LINEAR = 0, QUARTZ_ROTARY_BASE = 1, QUARTZ_ROTARY_PARTS = 2 };
+
+quartz_status quartz_rotary_frequencies(int64_t rot, double base, int32_t scaling, double factor,
+                                        double low, double high, double original, int64_t* freqs);
+
+quartz_status quartz_rotary(const void* x_bf16, void* y_bf16, int64_t tokens, int64_t heads,
+                            int64_t d, int64_t rot, int64_t x_token, int64_t x_head,
+                            int64_t y_token, int64_t y_head, const int32_t* positions,
+                            const int64_t* freqs, int32_t layout, int32_t inverse, float magnitude,
+                            hipStream_t stream);
+
+/*
+ * Paged cache of one layer's keys and values:
+ *   k_cache, v_cache  [pages][heads][page_size][d] of bf16 (QUARTZ_CACHE_BF16) or
+ *              OCP e4m3 (QUARTZ_CACHE_E4M3), page_stride elements from a page to
+ *              the next (at least heads page_size d; a multiple of 16 bytes).  A
+ *              stored value stands for itself times k_scale (v_scale), positive
+ *              and normal.  d is 64, 128 or 256, page_size a power of two from 8
+ *              to 4096.
+ *   table      int32 [rows][table_stride], table_pages entries used: entry j of
+ *              row s is the page of positions j page_size .. of sequence s; at
+ *              most 2^30 positions.  Entries outside [0, pages) are no page.
+ *
+ * quartz_paged_append: keys (turned on the way as by quartz_rotary, if rot > 0)
+ * and values of new tokens, k and v bf16 [tokens][heads][d] with any token and
+ * head strides, divided by the scales, rounded to nearest even (e4m3 saturates
+ * at 448), into the places of positions[t] of sequence sequences[t] (NULL: t).
+ * A token whose sequence is outside the table's rows, whose position is negative
+ * or past the table, or whose page is no page is skipped (padding).  Nothing
+ * else of the cache is written.  Two tokens of one place leave it with parts of
+ * either.
+ *
+ * quartz_paged_attention: for one new token of each sequence
+ *   o[b][h] = sum_j p_j v_j,  p = softmax over j of scale q[b][h] . k_j,
+ * over the positions j < lengths[b] of its pages, or the last `window` of them
+ * (window > 0); query head h reads cache head h / (heads / kv_heads).  lengths
+ * are clamped to [0, table_pages page_size]; positions without a page have no
+ * weight, and what the cache holds in places that do not count (infinities and
+ * NaN too) does not matter.  Without any key the output is 0.
+ *   q, o       bf16 [sequences][heads][d], strides in elements: multiples of 8
+ *              for q, of 4 for o (whose pointer needs 8-byte alignment).
+ *   table      row b belongs to sequence b (rows = sequences).
+ *   workspace  quartz_paged_attention_workspace_bytes of the same sizes (0: none
+ *              needed), any contents.  Calls that share one must not overlap in
+ *              time.
+ * The work is split by the table's width, not by the lengths (which the host
+ * does not read): a call may be captured into a graph and replayed with other
+ * lengths, pages and tokens.
+ */
+enum { QUARTZ_CACHE_BF16 = 0, QUARTZ_CACHE_E4M3 = 1 };
+
+quartz_status quartz_paged_append(const void* k_bf16, const void* v_bf16, int64_t tokens,
+                                  int64_t heads, int64_t d, int64_t k_token, int64_t k_head,
+                                  int64_t v_token, int64_t v_head, const int32_t* positions,
+                                  const int32_t* sequences, const int64_t* freqs, int64_t rot,
+                                  int32_t layout, float magnitude, void* k_cache, void* v_cache,
+                                  int32_t cache_type, float k_scale, float v_scale, int64_t pages,
+                                  int64_t page_size, int64_t page_stride, const int32_t* table,
+                                  int64_t table_rows, int64_t table_pages, int64_t table_stride,
+                                  hipStream_t stream);
+
+size_t quartz_paged_attention_workspace_bytes(int64_t sequences, int64_t heads, int64_t kv_heads,
+                                              int64_t d, int64_t page_size, int64_t table_pages,
+                                              int64_t window);
+
+quartz_status quartz_paged_attention(const void* q_bf16, void* o_bf16, int64_t sequences,
+                                     int64_t heads, int64_t kv_heads, int64_t d, int64_t q_token,
+                                     int64_t q_head, int64_t o_token, int64_t o_head,
+                                     const void* k_cache, const void* v_cache, int32_t cache_type,
+                                     float k_scale, float v_scale, int64_t pages, int64_t page_size,
+                                     int64_t page_stride, const int32_t* table, int64_t table_pages,
+                                     int64_t table_stride, const int32_t* lengths, float scale,
+                                     int64_t window, void* workspace, size_t workspace_bytes,
+                                     hipStream_t stream);
 
 /* Static, NUL-terminated description of a status code (host memory). */
 const char* quartz_status_string(quartz_status s);

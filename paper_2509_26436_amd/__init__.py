@@ -34,6 +34,13 @@ __all__ = [
     "quartz_attn_pv_workspace_bytes", "quartz_attn_pv", "quartz_lzs_attention_workspace_bytes",
     "quartz_lzs_attention", "quantize_vt", "attn_scores", "softmax_quantize", "attn_pv",
     "attention_workspace", "lzs_attention", "quartz_w4a4_layer_kernel", "layer_kernel",
+    "quartz_mxfp4_quantize", "quartz_mxfp4_dequantize", "quartz_mxfp4_linear",
+    "quartz_mxfp4_linear_workspace_bytes", "quartz_mxfp4_linear_bf16",
+    "quartz_rotary_frequencies", "quartz_rotary", "quartz_paged_append",
+    "quartz_paged_attention_workspace_bytes", "quartz_paged_attention",
+    "MxTensor", "PagedCache", "mxfp4_quantize", "mxfp4_dequantize", "mxfp4_linear",
+    "mxfp4_workspace", "rotary_frequencies", "rotary", "paged_append", "paged_attention",
+    "paged_attention_workspace",
 ]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -59,6 +66,10 @@ EXPORTED_SYMBOLS = (
     "quartz_quantize_vt", "quartz_attn_scores", "quartz_softmax_quantize",
     "quartz_attn_pv_workspace_bytes", "quartz_attn_pv", "quartz_lzs_attention_workspace_bytes",
     "quartz_lzs_attention", "quartz_w4a4_layer_kernel",
+    "quartz_mxfp4_quantize", "quartz_mxfp4_dequantize", "quartz_mxfp4_linear",
+    "quartz_mxfp4_linear_workspace_bytes", "quartz_mxfp4_linear_bf16",
+    "quartz_rotary_frequencies", "quartz_rotary", "quartz_paged_append",
+    "quartz_paged_attention_workspace_bytes", "quartz_paged_attention",
 )
 
 
@@ -152,6 +163,8 @@ def load() -> ctypes.CDLL:
     lib.quartz_lzs_attention.restype = I32
     lib.quartz_status_string.argtypes = [I32]
     lib.quartz_status_string.restype = ctypes.c_char_p
+    from . import decoding
+    decoding.bind(lib)
     _lib = lib
     return lib
 
@@ -802,3 +815,12 @@ def lzs_attention(q, k, v, heads: int, lzs_group: int = 16, out=None, workspace=
                               _stream_handle(stream))
     _check(st, "quartz_lzs_attention")
     return out
+
+
+from .decoding import (  # noqa: E402  (it uses the definitions above)
+    MxTensor, PagedCache, mxfp4_dequantize, mxfp4_linear, mxfp4_quantize, mxfp4_workspace,
+    paged_append, paged_attention, paged_attention_workspace, quartz_mxfp4_dequantize,
+    quartz_mxfp4_linear, quartz_mxfp4_linear_bf16, quartz_mxfp4_linear_workspace_bytes,
+    quartz_mxfp4_quantize, quartz_paged_append, quartz_paged_attention,
+    quartz_paged_attention_workspace_bytes, quartz_rotary, quartz_rotary_frequencies, rotary,
+    rotary_frequencies)

@@ -17,7 +17,8 @@ LIB = os.path.join(HERE, "libquartz.so")
 SOURCES = ["abi.hip", "quantize_lzs.hip", "pack_weight.hip", "w4a4_gemm.hip", "w4a4_linear.hip",
            "w4a4_gemm_plain.hip", "w4a4_linear_asym.hip", "w4a4_wide.hip", "w4a4_wide_modes.hip",
            "w4a4_wide_conv.hip", "w4a4_gemm_conv.hip", "scratch.hip",
-           "attention.hip", "attention_fused.hip"]
+           "attention.hip", "attention_fused.hip", "abi_decoding.hip", "mxfp4_quantize.hip",
+           "mxfp4_linear.hip", "rotary.hip", "paged_attention.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",

@@ -4,44 +4,26 @@
 #include <cfloat>
 #include <cmath>
 
+#include "abi_checks.h"
 #include "quartz.h"
 #include "quartz_internal.h"
 
+using quartz::aligned16;
+using quartz::from_hip;
+using quartz::kMaxK;
+using quartz::kMaxLd;
+using quartz::kMaxRowGroups;
+using quartz::size_ok;
+
 namespace {
 
-constexpr int64_t kMaxK = int64_t(1) << 20;       // at most 16384 groups per row
-// rows x groups of one call (M x K/64 or N x K/64): 2^34 elements, 32 GiB of
-// bf16 input; keeps every grid below 2^32 threads
-constexpr int64_t kMaxRowGroups = int64_t(1) << 28;
-// leading dimension of the activations and of the output (elements): 64 bf16
-// rows of it stay below 2^31 bytes (one buffer range per wave of output rows)
-constexpr int64_t kMaxLd = int64_t(1) << 24;
 // pixels of one implicit convolution (images * H * W): the GEMM addresses a
 // channel block's codes by pixel with 32-bit offsets (32 bytes per pixel)
 constexpr int64_t kMaxConvPixels = int64_t(1) << 26;
 
-// sizes that every entry point accepts: rows >= 0, 0 <= K <= kMaxK, K % 64 == 0
-// and rows * K / 64 <= kMaxRowGroups
-bool size_ok(int64_t rows, int64_t K)
-{
-    if (rows < 0 || K < 0 || K % 64 != 0 || K > kMaxK)
-        return false;
-    return K == 0 || rows <= kMaxRowGroups / (K / 64);
-}
-
-bool aligned16(const void* p)
-{
-    return (reinterpret_cast<uintptr_t>(p) & 15u) == 0;
-}
-
 bool lzs_ok(int32_t g)
 {
     return g == 8 || g == 16 || g == 32 || g == 64;
-}
-
-quartz_status from_hip(hipError_t e)
-{
-    return e == hipSuccess ? QUARTZ_OK : QUARTZ_ERR_HIP;
 }
 
 }  // namespace
@@ -58,13 +40,13 @@ const char* quartz_status_string(quartz_status s)
     case QUARTZ_ERR_SHAPE:
         return "invalid shape (negative size, K not a multiple of 64, leading dimension too small, or too large)";
     case QUARTZ_ERR_UNSUPPORTED:
-        return "unsupported group_size, lzs_group, mode or epilogue";
+        return "unsupported group_size, lzs_group, mode, epilogue or another option of the call";
     case QUARTZ_ERR_ALIGN:
-        return "a pointer is not 16-byte aligned";
+        return "a pointer or a stride is not aligned as the call needs it (base pointers: 16 bytes)";
     case QUARTZ_ERR_HIP:
         return "HIP kernel launch failed";
     case QUARTZ_ERR_WORKSPACE:
-        return "workspace smaller than quartz_w4a4_linear_workspace_bytes";
+        return "workspace missing or smaller than its size query asks for";
     }
     return "unknown status";
 }

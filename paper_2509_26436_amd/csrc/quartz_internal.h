@@ -261,6 +261,97 @@ hipError_t launch_attn_pv(const uint8_t* pc, const uint8_t* pf, const uint16_t* 
                           int lzs_group, uint16_t* o, int64_t ldo, const GemmSchedule& sch,
                           void* workspace, hipStream_t stream);
 
+// ------------------------------------------------------------ MXFP4
+// mxfp4.h has the format and the layout of codes and scales.
+hipError_t launch_mxfp4_quantize(const uint16_t* x, int64_t M, int64_t K, int64_t ldx, uint8_t* codes,
+                                 uint8_t* scales, hipStream_t stream);
+hipError_t launch_mxfp4_dequantize(const uint8_t* codes, const uint8_t* scales, int64_t M, int64_t K,
+                                   uint16_t* y, int64_t ldy, hipStream_t stream);
+// y [M][ldy] = act(A W^T + bias); A either in MXFP4 (x_codes, x_scales) or, if
+// mxfp4_fuses(M), in bf16 (x [M][ldx], quantized within the kernel).
+struct MxLinear {
+    const uint16_t* x;
+    int64_t ldx;
+    const uint8_t* x_codes;
+    const uint8_t* x_scales;
+    const uint8_t* w_codes;
+    const uint8_t* w_scales;
+    const uint16_t* bias;     // may be nullptr
+    uint16_t* y;
+    int64_t M, N, K, ldy;
+    bool gelu;
+};
+bool mxfp4_fuses(int64_t M);
+hipError_t launch_mxfp4_linear(const MxLinear& a, hipStream_t stream);
+
+// ------------------------------------------------------------ decoding
+// Rotary positions of tokens x heads x d (strides in elements); pairs of the
+// first `rot` channels, freqs [rot / 2] in turns of 2^-64 a position.
+struct Rotary {
+    const uint16_t* x;
+    uint16_t* y;              // may be x, with the same strides
+    int64_t tokens;
+    int32_t heads, d, rot;
+    int64_t x_token, x_head, y_token, y_head;
+    const int32_t* positions;
+    const int64_t* freqs;
+    bool interleaved, inverse;
+    float magnitude;
+};
+hipError_t launch_rotary(const Rotary& a, hipStream_t stream);
+
+// A layer's paged cache: k and v [pages][heads][page][d] of bf16 or e4m3
+// (page_stride elements from a page to the next), a stored value standing for
+// itself times the scale; row s of the table [sequences][table_stride] holds
+// the pages of sequence s.
+struct PagedCacheView {
+    void* k;
+    void* v;
+    int64_t pages, page_stride;
+    int32_t heads, d, page_shift;
+    bool fp8;
+    float k_scale, v_scale;
+    const int32_t* table;
+    int64_t sequences, table_stride;
+    int32_t table_pages;
+};
+
+struct PagedAppend {
+    PagedCacheView cache;
+    const uint16_t* k;
+    const uint16_t* v;
+    int64_t tokens, k_token, k_head, v_token, v_head;
+    const int32_t* positions;
+    const int32_t* sequences; // nullptr: token t is of sequence t
+    const int64_t* freqs;
+    int32_t rot;              // 0: keys are not turned
+    bool interleaved;
+    float magnitude;
+};
+hipError_t launch_paged_append(const PagedAppend& a, hipStream_t stream);
+
+// One new token a sequence: o [sequences][heads][d] from q.
+struct PagedAttention {
+    PagedCacheView cache;     // .sequences: the batch
+    const uint16_t* q;
+    uint16_t* o;
+    int64_t q_token, q_head, o_token, o_head;
+    int32_t heads;            // of q: a multiple of cache.heads
+    const int32_t* lengths;
+    float scale;
+    int32_t window;           // 0: all keys
+    int32_t split_keys;       // from paged_split
+    int32_t splits;
+    float* workspace;         // paged_attention_workspace_bytes
+};
+// keys a block takes and the number of blocks along the longest sequence
+struct PagedSplit {
+    int32_t keys, splits;
+};
+PagedSplit paged_split(int64_t sequences, int64_t heads, int64_t kv_heads, int64_t d, int64_t longest);
+size_t paged_attention_bytes(int64_t sequences, int64_t heads, int64_t d, const PagedSplit& s);
+hipError_t launch_paged_attention(const PagedAttention& a, hipStream_t stream);
+
 // ------------------------------------------------------------ device helpers
 
 // Nibble word -> 8 OCP fp8 e4m3 bytes of (+-|c|) * 2^flag.
