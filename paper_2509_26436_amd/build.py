@@ -1,4 +1,5 @@
-"""Build libquartz.so in-tree with hipcc for gfx950.
+"""Build libquartz.so in-tree with hipcc for gfx950, and the compiled half of the decoding
+helpers (_decoding.so, host code on torch's C++ API) with g++.
 
 Every HIP source is compiled with fp contraction off (the quantizer's
 products must round to fp32 before the half-even rounding) and without
@@ -14,6 +15,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libquartz.so")
+BINDING = os.path.join(HERE, "_decoding.so")
+BINDING_SOURCE = "decoding_binding.cpp"
 SOURCES = ["abi.hip", "quantize_lzs.hip", "pack_weight.hip", "w4a4_gemm.hip", "w4a4_linear.hip",
            "w4a4_gemm_plain.hip", "w4a4_linear_asym.hip", "w4a4_wide.hip", "w4a4_wide_modes.hip",
            "w4a4_wide_conv.hip", "w4a4_gemm_conv.hip", "scratch.hip",
@@ -33,43 +36,68 @@ def hipcc() -> str:
     return os.path.join(rocm, "bin", "hipcc")
 
 
+def binding_flags() -> tuple[list, list]:
+    """g++ flags (compile, link) of the binding: the installed torch's headers and libraries."""
+    import sysconfig
+
+    import torch
+    base = os.path.dirname(torch.__file__)
+    rocm = os.environ.get("ROCM_PATH", "/opt/rocm")
+    compile_flags = ["-O2", "-std=c++17", "-fPIC", "-D__HIP_PLATFORM_AMD__", "-DUSE_ROCM",
+                     f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+                     "-isystem", os.path.join(base, "include"),
+                     "-isystem", os.path.join(base, "include", "torch", "csrc", "api", "include"),
+                     "-isystem", os.path.join(rocm, "include"),
+                     "-isystem", sysconfig.get_paths()["include"], "-Wall"]
+    link_flags = ["-L", os.path.join(base, "lib"), "-lc10", "-lc10_hip", "-ltorch_cpu", "-ltorch_python",
+                  "-L", HERE, "-lquartz", "-Wl,-rpath,$ORIGIN"]
+    return compile_flags, link_flags
+
+
 def build(verbose: bool = False) -> str:
     """Compile every source to an object in parallel (each GEMM output mode is
-    its own translation unit), then link libquartz.so."""
+    its own translation unit), then link libquartz.so and the binding."""
     import concurrent.futures
     import tempfile
 
     noise = "is not a recognized feature for this target"
     inc = ["-I", os.path.join(ROOT, "include"), "-I", CSRC]
     compile_flags = [f for f in HIPCC_FLAGS if f != "-shared"]
+    binding_compile, binding_link = binding_flags()
     with tempfile.TemporaryDirectory(prefix="quartz_build_") as tmpdir:
         def compile_one(src):
             obj = os.path.join(tmpdir, os.path.splitext(src)[0] + ".o")
-            cmd = [hipcc(), *compile_flags, *inc, "-c", "-o", obj, os.path.join(CSRC, src)]
+            compiler = ["g++", *binding_compile] if src == BINDING_SOURCE else [hipcc(), *compile_flags]
+            cmd = [*compiler, *inc, "-c", "-o", obj, os.path.join(CSRC, src)]
             if verbose:
                 print(" ".join(cmd), flush=True)
             res = subprocess.run(cmd, capture_output=True, text=True)
             err = "\n".join(l for l in res.stderr.splitlines() if noise not in l)
             return src, obj, res.returncode, err
 
-        workers = max(1, min(len(SOURCES), os.cpu_count() or 1))
+        sources = [*SOURCES, BINDING_SOURCE]
+        workers = max(1, min(len(sources), os.cpu_count() or 1))
         with concurrent.futures.ThreadPoolExecutor(max_workers=workers) as ex:
-            results = list(ex.map(compile_one, SOURCES))
+            results = list(ex.map(compile_one, sources))
         failed = [r for r in results if r[2] != 0]
         for src, _, _, err in results:
             if err.strip() and (verbose or failed):
                 sys.stderr.write(f"{src}:\n{err}\n")
         if failed:
-            raise RuntimeError("hipcc failed building libquartz.so: " +
+            raise RuntimeError("compiling libquartz.so or its binding failed: " +
                                ", ".join(r[0] for r in failed))
-        tmp = LIB + ".tmp"
-        cmd = [hipcc(), "--offload-arch=gfx950", "-shared", "-fPIC", "-o", tmp,
-               *[r[1] for r in results]]
-        res = subprocess.run(cmd, capture_output=True, text=True)
-        if res.returncode != 0:
-            sys.stderr.write(res.stderr + "\n")
-            raise RuntimeError("linking libquartz.so failed")
-    os.replace(tmp, LIB)
+        objects = {r[0]: r[1] for r in results}
+        binding = objects.pop(BINDING_SOURCE)
+
+        def link(target, cmd):
+            tmp = target + ".tmp"
+            res = subprocess.run([*cmd, "-o", tmp], capture_output=True, text=True)
+            if res.returncode != 0:
+                sys.stderr.write(res.stderr + "\n")
+                raise RuntimeError(f"linking {os.path.basename(target)} failed")
+            os.replace(tmp, target)
+        link(LIB, [hipcc(), "--offload-arch=gfx950", "-shared", "-fPIC", *objects.values()])
+        link(BINDING, ["g++", "-shared", "-fPIC", binding, *binding_link])
     return LIB
 
 

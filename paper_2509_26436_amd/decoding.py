@@ -2,21 +2,18 @@
 and attention of one new token a sequence over a paged cache (include/quartz.h, "decoding").
 
 As in the rest of the package, the functions named like the C entry points take raw integers and
-return the status code; the tensor helpers check their tensors, allocate outputs on the inputs'
-device (and on ``stream``, where one is given) and raise ``QuartzError`` on a non-OK status.  They
-launch on the inputs' device, whichever device is current.
+return the status code; the tensor helpers check their tensors (``ValueError``), allocate outputs on
+the inputs' device (as memory of ``stream``, where one is given) and raise ``QuartzError`` on a
+non-OK status.  They launch on the inputs' device, whichever device is current.  The helpers'
+marshalling is compiled: a decoding step is many calls of a few microseconds.
 """
 from __future__ import annotations
 
 import ctypes
-import math
-from dataclasses import dataclass
 
 import paper_2509_26436_amd as _q
 
-ROTARY_LAYOUTS = ("half", "interleaved")
 ROTARY_SCALINGS = ("linear", "base", "parts")
-CACHE_BF16, CACHE_E4M3 = 0, 1
 
 P, I64, I32, F32, F64, SZ = (ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32, ctypes.c_float,
                              ctypes.c_double, ctypes.c_size_t)
@@ -108,113 +105,72 @@ def quartz_paged_attention(q, o, sequences, heads, kv_heads, d, q_token, q_head,
 
 # ------------------------------------------------------------------- tensor helpers
 
-def _need(ok: bool, what: str):
-    if not ok:
-        raise ValueError(what)
+_native_module = None
 
 
-def _same_device(device, *tensors):
-    for t in tensors:
-        if t is not None and t.device != device:
-            raise ValueError(f"all tensors must be on one device: {t.device} beside {device}")
+def _native():
+    """The compiled half of the helpers (csrc/decoding_binding.cpp); raises if it is missing."""
+    global _native_module
+    if _native_module is None:
+        _q._torch()
+        _q.load()
+        try:
+            from . import _decoding
+        except ImportError as e:
+            raise RuntimeError("the compiled binding _decoding.so is missing or does not load; build it "
+                               "with `python paper_2509_26436_amd/build.py`") from e
+        _native_module = _decoding
+    return _native_module
 
 
-def _empty(shape, dtype, device, stream):
-    """An output: memory of the stream that writes it."""
-    torch = _q._torch()
-    if stream is None:
-        return torch.empty(shape, dtype=dtype, device=device)
-    with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device=device)
+class _On:
+    """The stream a call was given, as the current one (its device too)."""
+
+    def __init__(self, stream, tensor):
+        if tensor.device != stream.device:
+            raise ValueError(f"the stream is of {stream.device}, the tensors are on {tensor.device}")
+        self._context = _q._torch().cuda.stream(stream)
+
+    def __enter__(self):
+        self._context.__enter__()
+
+    def __exit__(self, *error):
+        self._context.__exit__(*error)
 
 
-def _call(name: str, device, stream, *args):
-    """The entry point on the tensors' device: the given stream, or that device's current one."""
-    if device.type != "cuda":
-        raise ValueError(f"{name}: the tensors must be on a GPU, not on {device}")
-    torch = _q._torch()
-    f = getattr(_q.load(), name)
-    index = device.index
-    if stream is None:
-        handle = torch._C._cuda_getCurrentRawStream(index)
-    else:
-        _need(stream.device == device, f"the stream is of {stream.device}, the tensors are on {device}")
-        handle = stream.cuda_stream
-    if torch._C._cuda_getDevice() == index:
-        status = f(*args, handle)
-    else:
-        with torch.cuda.device(index):
-            status = f(*args, handle)
-    if status:
-        raise _q.QuartzError(status, name)
-
-
-def _rows(t, what: str):
-    """Rows, columns and leading dimension of a bf16 matrix with unit column stride."""
-    torch = _q._torch()
-    if t.dtype != torch.bfloat16 or t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
-        raise ValueError(f"{what} must be a 2-D bf16 tensor with unit column stride")
-    M, K = t.shape
-    return M, K, (t.stride(0) if M > 1 else -(-K // 8) * 8)
-
-
-def _epilogue_out(M: int, N: int, bias, out, device, stream):
-    torch = _q._torch()
-    if bias is not None and (bias.dtype != torch.bfloat16 or bias.shape != (N,) or
-                             (bias.stride(0) != 1 and N > 1)):
-        raise ValueError("bias must be bf16 [N], contiguous")
-    if out is None:
-        return _empty((M, N), torch.bfloat16, device, stream), N
-    rows, columns, ldy = _rows(out, "out")
-    _need(rows == M and columns >= N, "out must be bf16 [M, >= N]")
-    return out, (ldy if M > 1 else max(ldy, N))
-
-
-@dataclass(frozen=True)
 class MxTensor:
     """An MXFP4 tensor of ``rows`` x ``K`` (include/quartz.h has the format): activations, or a
-    linear layer's weight [N, K]."""
-    codes: "object"     # uint8 [K/32, rows, 16]
-    scales: "object"    # uint8 [ceil(K/128), rows, 4]
-    rows: int
-    K: int
+    linear layer's weight [N, K].  ``codes``: uint8 [K/32, rows, 16], ``scales``: uint8
+    [ceil(K/128), rows, 4]."""
+    __slots__ = ("codes", "scales", "rows", "K")
 
-    def __post_init__(self):
-        torch, c, s = _q._torch(), self.codes, self.scales
-        _need(self.K % 64 == 0, "K must be a multiple of 64")
-        _need(c.dtype == s.dtype == torch.uint8 and c.shape == (self.K // 32, self.rows, 16) and
-              s.shape == (-(-self.K // 128), self.rows, 4) and c.is_contiguous() and s.is_contiguous(),
-              "codes must be contiguous uint8 [K/32, rows, 16], scales contiguous uint8 [ceil(K/128), rows, 4]")
-        _same_device(c.device, s)
+    def __init__(self, codes, scales, rows: int, K: int):
+        _native().check_mx(codes, scales, rows, K)
+        self.codes, self.scales, self.rows, self.K = codes, scales, rows, K
+
+    def __repr__(self):
+        return f"MxTensor({self.rows} x {self.K}, {self.codes.device})"
 
 
 def mxfp4_quantize(x, out: MxTensor | None = None, stream=None) -> MxTensor:
     """bf16 [M, K] (unit column stride, K a multiple of 64, 16-byte aligned rows) to MXFP4:
     activations, or a weight [N, K] once per layer."""
-    M, K, ldx = _rows(x, "x")
+    if stream is not None:
+        with _On(stream, x):
+            return mxfp4_quantize(x, out)
     if out is None:
-        _need(K % 64 == 0, "K must be a multiple of 64")
-        uint8 = _q._torch().uint8
-        out = MxTensor(_empty((K // 32, M, 16), uint8, x.device, stream),
-                       _empty((-(-K // 128), M, 4), uint8, x.device, stream), M, K)
-    _need(out.rows == M and out.K == K, "out must have x's rows and K")
-    _same_device(x.device, out.codes)
-    _call("quartz_mxfp4_quantize", x.device, stream, x.data_ptr(), M, K, ldx, out.codes.data_ptr(),
-          out.scales.data_ptr())
+        codes, scales = _native().quantize_new(x)
+        return MxTensor(codes, scales, *x.shape)
+    _native().quantize_into(x, out.codes, out.scales, out.rows, out.K)
     return out
 
 
 def mxfp4_dequantize(t: MxTensor, out=None, stream=None):
     """The bf16 values [rows, K] that an MXFP4 tensor stands for."""
-    M, K, device = t.rows, t.K, t.codes.device
-    if out is None:
-        out = _empty((M, K), _q._torch().bfloat16, device, stream)
-    rows, columns, ldy = _rows(out, "out")
-    _need(rows == M and columns == K, "out must be bf16 [rows, K]")
-    _same_device(device, out)
-    _call("quartz_mxfp4_dequantize", device, stream, t.codes.data_ptr(), t.scales.data_ptr(), M, K,
-          out.data_ptr(), ldy)
-    return out
+    if stream is not None:
+        with _On(stream, t.codes):
+            return mxfp4_dequantize(t, out)
+    return _native().dequantize(t.codes, t.scales, t.rows, t.K, out)
 
 
 def mxfp4_workspace(M: int, K: int, device):
@@ -228,31 +184,13 @@ def mxfp4_linear(x, w: MxTensor, bias=None, epilogue: int = 0, out=None, stream=
     activations [M, K], which the call quantizes (into ``workspace`` from ``mxfp4_workspace``, else
     one of its own; few tokens need none).  Writes ``out``, a bf16 [M, >= N] view with unit column
     stride, if given."""
-    N, K, device = w.rows, w.K, w.codes.device
-    b = None if bias is None else bias.data_ptr()
+    if stream is not None:
+        with _On(stream, w.codes):
+            return mxfp4_linear(x, w, bias, epilogue, out, None, workspace)
     if isinstance(x, MxTensor):
-        _need(x.K == K, "K mismatch between activations and weights")
-        _same_device(device, x.codes, bias, out)
-        out, ldy = _epilogue_out(x.rows, N, bias, out, device, stream)
-        _call("quartz_mxfp4_linear", device, stream, x.codes.data_ptr(), x.scales.data_ptr(),
-              w.codes.data_ptr(), w.scales.data_ptr(), b, out.data_ptr(), x.rows, N, K, ldy, epilogue)
-        return out
-    M, columns, ldx = _rows(x, "x")
-    _need(columns == K, "K mismatch between activations and weights")
-    _same_device(device, x, bias, out, workspace)
-    out, ldy = _epilogue_out(M, N, bias, out, device, stream)
-    n = 0
-    if workspace is None:
-        n = _q.load().quartz_mxfp4_linear_workspace_bytes(M, K)
-        if n:
-            workspace = _empty((n,), _q._torch().uint8, device, stream)
-    else:
-        _need(workspace.is_contiguous(), "the workspace must be contiguous")
-        n = workspace.numel() * workspace.element_size()
-    _call("quartz_mxfp4_linear_bf16", device, stream, x.data_ptr(), ldx, w.codes.data_ptr(),
-          w.scales.data_ptr(), b, out.data_ptr(), M, N, K, ldy, epilogue,
-          None if workspace is None else workspace.data_ptr(), n)
-    return out
+        return _native().linear_mx(x.codes, x.scales, x.rows, x.K, w.codes, w.scales, w.rows, w.K, bias,
+                                   epilogue, out)
+    return _native().linear_bf16(x, w.codes, w.scales, w.rows, w.K, bias, epilogue, out, workspace)
 
 
 def rotary_frequencies(rot: int, base: float = 10000.0, scaling: str = "linear", factor: float = 1.0,
@@ -261,7 +199,8 @@ def rotary_frequencies(rot: int, base: float = 10000.0, scaling: str = "linear",
     turns a position in units of 2^-64, on ``device``.  ``scaling`` and ``factor`` stretch them for
     longer contexts (quartz_rotary_frequencies; low, high and original belong to "parts")."""
     torch = _q._torch()
-    _need(scaling in ROTARY_SCALINGS, f"scaling must be one of {ROTARY_SCALINGS}")
+    if scaling not in ROTARY_SCALINGS:
+        raise ValueError(f"scaling must be one of {ROTARY_SCALINGS}")
     host = torch.empty((max(rot, 0) // 2,), dtype=torch.int64)
     status = quartz_rotary_frequencies(rot, base, ROTARY_SCALINGS.index(scaling), factor, low, high,
                                        original, host.data_ptr())
@@ -270,81 +209,28 @@ def rotary_frequencies(rot: int, base: float = 10000.0, scaling: str = "linear",
     return host.to(device)
 
 
-def _heads(t, what: str):
-    """[tokens, heads, d] bf16 with unit stride along d -> its sizes and strides."""
-    if t.dtype != _q._torch().bfloat16 or t.dim() != 3 or (t.stride(2) != 1 and t.shape[2] > 1):
-        raise ValueError(f"{what} must be a bf16 [tokens, heads, d] tensor with unit stride along d")
-    return t.shape, t.stride()
-
-
-def _int32(t, n: int, what: str):
-    if t.dtype != _q._torch().int32 or t.shape != (n,) or (t.stride(0) != 1 and n > 1):
-        raise ValueError(f"{what} must be a contiguous int32 tensor of {n}")
-
-
-def _freqs(freqs, layout: str, d: int):
-    if freqs.dtype != _q._torch().int64 or freqs.dim() != 1 or not freqs.is_contiguous() or \
-            2 * freqs.shape[0] > d:
-        raise ValueError("freqs must be a contiguous int64 tensor of at most d / 2 (rotary_frequencies)")
-    _need(layout in ROTARY_LAYOUTS, f"layout must be one of {ROTARY_LAYOUTS}")
-    return 2 * freqs.shape[0], ROTARY_LAYOUTS.index(layout)
-
-
 def rotary(x, positions, freqs, layout: str = "half", inverse: bool = False, magnitude: float = 1.0,
            out=None, stream=None):
     """Rotary positions on x bf16 [tokens, heads, d] (any token and head strides): the first
     2 len(freqs) channels of every head turned by its token's position, the others copied.
-    ``positions``: int32 [tokens].  ``inverse=True`` is the transposed map: it takes the gradient of
+    ``positions``: int32 [tokens].  ``layout`` pairs channels: "half" (i, i + len(freqs)) or
+    "interleaved" (2i, 2i + 1).  ``inverse=True`` is the transposed map: it takes the gradient of
     the output to that of the input.  ``out`` may be x."""
-    (tokens, heads, d), (x_token, x_head, _) = _heads(x, "x")
-    _int32(positions, tokens, "positions")
-    rot, kind = _freqs(freqs, layout, d)
-    if out is None:
-        if stream is None:
-            out = _q._torch().empty_like(x)
-        else:
-            with _q._torch().cuda.stream(stream):
-                out = _q._torch().empty_like(x)
-    shape, (y_token, y_head, _) = _heads(out, "out")
-    _need(shape == x.shape, "out must have x's shape")
-    _same_device(x.device, positions, freqs, out)
-    _call("quartz_rotary", x.device, stream, x.data_ptr(), out.data_ptr(), tokens, heads, d, rot, x_token,
-          x_head, y_token, y_head, positions.data_ptr(), freqs.data_ptr(), kind, int(inverse), magnitude)
-    return out
+    if stream is not None:
+        with _On(stream, x):
+            return rotary(x, positions, freqs, layout, inverse, magnitude, out)
+    return _native().rotary(x, positions, freqs, layout, inverse, magnitude, out)
 
 
-@dataclass(frozen=True)
 class PagedCache:
     """A layer's keys and values in pages, [pages, heads, page_size, d] of bf16 or float8_e4m3fn
     (pages may be strided), and the sequences' page table, int32 [sequences, pages of the longest].
     A stored value stands for itself times its scale."""
-    k: "object"
-    v: "object"
-    table: "object"
-    k_scale: float = 1.0
-    v_scale: float = 1.0
+    __slots__ = ("k", "v", "table", "k_scale", "v_scale")
 
-    def __post_init__(self):
-        torch, k, v, table = _q._torch(), self.k, self.v, self.table
-        _need(k.dtype in (torch.bfloat16, torch.float8_e4m3fn) and v.dtype == k.dtype,
-              "k and v must both be bf16 or both float8_e4m3fn")
-        _need(k.dim() == 4 and k.shape == v.shape, "k and v must be [pages, heads, page_size, d], both alike")
-        for t in (k, v):
-            _need(t.is_contiguous() or (t.shape[0] > 0 and t[0].is_contiguous() and t.stride() == k.stride()),
-                  "a page must be contiguous, and k and v must have one page stride")
-        if k.stride(0) != v.stride(0):
-            _need(k.shape[0] == 1, "k and v must have one page stride")
-        _need(table.dtype == torch.int32 and table.dim() == 2 and
-              (table.stride(1) == 1 or table.shape[1] <= 1),
-              "table must be an int32 [sequences, pages] tensor with unit column stride")
-        _same_device(k.device, v, table)
-
-    def _page_stride(self):
-        pages, heads, page, d = self.k.shape
-        return self.k.stride(0) if pages > 1 else heads * page * d
-
-    def _type(self):
-        return CACHE_BF16 if self.k.dtype == _q._torch().bfloat16 else CACHE_E4M3
+    def __init__(self, k, v, table, k_scale: float = 1.0, v_scale: float = 1.0):
+        _native().check_cache(k, v, table, k_scale, v_scale)
+        self.k, self.v, self.table, self.k_scale, self.v_scale = k, v, table, k_scale, v_scale
 
 
 def paged_append(cache: PagedCache, k, v, positions, sequences=None, freqs=None, layout: str = "half",
@@ -353,22 +239,11 @@ def paged_append(cache: PagedCache, k, v, positions, sequences=None, freqs=None,
     strides), into the places of ``positions`` (int32 [tokens]) of ``sequences`` (int32 [tokens],
     rows of the table; None: token t is of sequence t).  ``freqs`` turns the keys on the way, as
     ``rotary`` does.  Tokens without a place (negative positions, pages that are none) are skipped."""
-    (tokens, heads, d), (k_token, k_head, _) = _heads(k, "k")
-    shape, (v_token, v_head, _) = _heads(v, "v")
-    pages, cache_heads, page, cache_d = cache.k.shape
-    _need(shape == k.shape and heads == cache_heads and d == cache_d,
-          "k and v must be [tokens, heads, d] with the cache's heads and d")
-    _int32(positions, tokens, "positions")
-    if sequences is not None:
-        _int32(sequences, tokens, "sequences")
-    rot, kind = (0, 0) if freqs is None else _freqs(freqs, layout, d)
-    table = cache.table
-    _same_device(cache.k.device, k, v, positions, sequences, freqs)
-    _call("quartz_paged_append", cache.k.device, stream, k.data_ptr(), v.data_ptr(), tokens, heads, d, k_token,
-          k_head, v_token, v_head, positions.data_ptr(), None if sequences is None else sequences.data_ptr(),
-          None if freqs is None else freqs.data_ptr(), rot, kind, magnitude, cache.k.data_ptr(),
-          cache.v.data_ptr(), cache._type(), cache.k_scale, cache.v_scale, pages, page, cache._page_stride(),
-          table.data_ptr(), table.shape[0], table.shape[1], max(table.stride(0), table.shape[1]))
+    if stream is not None:
+        with _On(stream, k):
+            return paged_append(cache, k, v, positions, sequences, freqs, layout, magnitude)
+    _native().append(cache.k, cache.v, cache.table, cache.k_scale, cache.v_scale, k, v, positions, sequences,
+                     freqs, layout, magnitude)
 
 
 def paged_attention_workspace(sequences: int, heads: int, cache: PagedCache, window: int = 0):
@@ -386,30 +261,8 @@ def paged_attention(q, cache: PagedCache, lengths, scale: float | None = None, w
     GPU) positions of its pages, or the last ``window`` of them: q bf16 [sequences, heads, d] ->
     bf16 [sequences, heads, d].  heads is a multiple of the cache's heads (neighbouring query heads
     share one); ``scale`` is 1 / sqrt(d) by default.  A sequence of length 0 gives zeros."""
-    (sequences, heads, d), (q_token, q_head, _) = _heads(q, "q")
-    pages, kv_heads, page, cache_d = cache.k.shape
-    table, device = cache.table, cache.k.device
-    _need(d == cache_d and table.shape[0] == sequences and kv_heads > 0 and heads % kv_heads == 0,
-          "q must be [sequences, heads, d] with the cache's d, a row of the table a sequence, and "
-          "heads a multiple of the cache's")
-    _int32(lengths, sequences, "lengths")
-    if out is None:
-        out = _empty((sequences, heads, d), q.dtype, q.device, stream)
-    shape, (o_token, o_head, _) = _heads(out, "out")
-    _need(shape == q.shape, "out must have q's shape")
-    _same_device(device, q, lengths, out, workspace)
-    if workspace is None:
-        n = _q.load().quartz_paged_attention_workspace_bytes(sequences, heads, kv_heads, d, page,
-                                                             table.shape[1], window)
-        if n:
-            workspace = _empty((n,), _q._torch().uint8, device, stream)
-    else:
-        _need(workspace.is_contiguous(), "the workspace must be contiguous")
-        n = workspace.numel() * workspace.element_size()
-    _call("quartz_paged_attention", device, stream, q.data_ptr(), out.data_ptr(), sequences, heads, kv_heads, d,
-          q_token, q_head, o_token, o_head, cache.k.data_ptr(), cache.v.data_ptr(), cache._type(),
-          cache.k_scale, cache.v_scale, pages, page, cache._page_stride(), table.data_ptr(), table.shape[1],
-          max(table.stride(0), table.shape[1]), lengths.data_ptr(),
-          1.0 / math.sqrt(d) if scale is None else scale, window,
-          None if workspace is None else workspace.data_ptr(), n)
-    return out
+    if stream is not None:
+        with _On(stream, q):
+            return paged_attention(q, cache, lengths, scale, window, out, workspace)
+    return _native().attention(cache.k, cache.v, cache.table, cache.k_scale, cache.v_scale, q, lengths, scale,
+                               window, out, workspace)
