@@ -573,7 +573,14 @@ int64_t quartz_w4a4_linear_schedule(int64_t M, int64_t N, int64_t K, int32_t blo
  *   workspace (that many bytes, 16-byte aligned, any contents).
  *   QUARTZ_ERR_WORKSPACE if it is missing or smaller.  Calls that share a
  *   workspace must not overlap in time.
+ * quartz_mxfp4_linear_kernel (host only, needs no GPU): the kernel that a layer
+ *   of these sizes launches: host int32[4] of QUARTZ_MX_*, the tokens and columns
+ *   of its tiles, and 1 if quartz_mxfp4_linear_bf16 quantizes within the kernel
+ *   (which then is QUARTZ_MX_DIRECT).
  */
+#define QUARTZ_MX_DIRECT 0
+#define QUARTZ_MX_TILED 1
+
 quartz_status quartz_mxfp4_quantize(const void* x_bf16, int64_t M, int64_t K, int64_t ldx,
                                     uint8_t* codes, uint8_t* scales, hipStream_t stream);
 
@@ -592,6 +599,8 @@ quartz_status quartz_mxfp4_linear_bf16(const void* x_bf16, int64_t ldx, const ui
                                        int64_t M, int64_t N, int64_t K, int64_t ldy,
                                        int32_t epilogue, void* workspace, size_t workspace_bytes,
                                        hipStream_t stream);
+
+quartz_status quartz_mxfp4_linear_kernel(int64_t M, int64_t N, int64_t K, int32_t* kernel);
 
 /*
  * Rotary positions: pair i < rot / 2 of a head at position p is turned by p f_i

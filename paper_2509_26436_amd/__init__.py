@@ -35,11 +35,11 @@ __all__ = [
     "quartz_lzs_attention", "quantize_vt", "attn_scores", "softmax_quantize", "attn_pv",
     "attention_workspace", "lzs_attention", "quartz_w4a4_layer_kernel", "layer_kernel",
     "quartz_mxfp4_quantize", "quartz_mxfp4_dequantize", "quartz_mxfp4_linear",
-    "quartz_mxfp4_linear_workspace_bytes", "quartz_mxfp4_linear_bf16",
+    "quartz_mxfp4_linear_workspace_bytes", "quartz_mxfp4_linear_bf16", "quartz_mxfp4_linear_kernel",
     "quartz_rotary_frequencies", "quartz_rotary", "quartz_paged_append",
     "quartz_paged_attention_workspace_bytes", "quartz_paged_attention",
     "MxTensor", "PagedCache", "mxfp4_quantize", "mxfp4_dequantize", "mxfp4_linear",
-    "mxfp4_workspace", "rotary_frequencies", "rotary", "paged_append", "paged_attention",
+    "mxfp4_workspace", "mxfp4_linear_kernel", "rotary_frequencies", "rotary", "paged_append", "paged_attention",
     "paged_attention_workspace",
 ]
 
@@ -67,7 +67,7 @@ EXPORTED_SYMBOLS = (
     "quartz_attn_pv_workspace_bytes", "quartz_attn_pv", "quartz_lzs_attention_workspace_bytes",
     "quartz_lzs_attention", "quartz_w4a4_layer_kernel",
     "quartz_mxfp4_quantize", "quartz_mxfp4_dequantize", "quartz_mxfp4_linear",
-    "quartz_mxfp4_linear_workspace_bytes", "quartz_mxfp4_linear_bf16",
+    "quartz_mxfp4_linear_workspace_bytes", "quartz_mxfp4_linear_bf16", "quartz_mxfp4_linear_kernel",
     "quartz_rotary_frequencies", "quartz_rotary", "quartz_paged_append",
     "quartz_paged_attention_workspace_bytes", "quartz_paged_attention",
 )
@@ -818,9 +818,10 @@ def lzs_attention(q, k, v, heads: int, lzs_group: int = 16, out=None, workspace=
 
 
 from .decoding import (  # noqa: E402  (it uses the definitions above)
-    MxTensor, PagedCache, mxfp4_dequantize, mxfp4_linear, mxfp4_quantize, mxfp4_workspace,
-    paged_append, paged_attention, paged_attention_workspace, quartz_mxfp4_dequantize,
-    quartz_mxfp4_linear, quartz_mxfp4_linear_bf16, quartz_mxfp4_linear_workspace_bytes,
+    MxTensor, PagedCache, mxfp4_dequantize, mxfp4_linear, mxfp4_linear_kernel, mxfp4_quantize,
+    mxfp4_workspace, paged_append, paged_attention, paged_attention_workspace,
+    quartz_mxfp4_dequantize, quartz_mxfp4_linear, quartz_mxfp4_linear_bf16,
+    quartz_mxfp4_linear_kernel, quartz_mxfp4_linear_workspace_bytes,
     quartz_mxfp4_quantize, quartz_paged_append, quartz_paged_attention,
     quartz_paged_attention_workspace_bytes, quartz_rotary, quartz_rotary_frequencies, rotary,
     rotary_frequencies)

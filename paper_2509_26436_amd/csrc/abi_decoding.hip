@@ -140,7 +140,7 @@ quartz_status quartz_mxfp4_linear(const uint8_t* a_codes, const uint8_t* a_scale
 
 size_t quartz_mxfp4_linear_workspace_bytes(int64_t M, int64_t K)
 {
-    if (M <= 0 || K <= 0 || !size_ok(M, K) || mxfp4_fuses(M))
+    if (M <= 0 || K <= 0 || !size_ok(M, K) || mxfp4_fuses(M, K))
         return 0;
     return mx_workspace(M, K).total;
 }
@@ -159,7 +159,7 @@ quartz_status quartz_mxfp4_linear_bf16(const void* x_bf16, int64_t ldx, const ui
         return QUARTZ_ERR_ALIGN;
     if (M == 0 || N == 0)
         return QUARTZ_OK;
-    const bool fused = mxfp4_fuses(M);
+    const bool fused = mxfp4_fuses(M, K);
     if (!x_bf16 || !w_codes || !w_scales || !y_bf16)
         return QUARTZ_ERR_NULL;
     if (!aligned16(x_bf16) || !aligned16(w_codes) || !aligned16(w_scales) || !aligned16(y_bf16) ||
@@ -181,6 +181,24 @@ quartz_status quartz_mxfp4_linear_bf16(const void* x_bf16, int64_t ldx, const ui
         a.x_scales = codes + w.scales;
     }
     return from_hip(launch_mxfp4_linear(a, stream));
+}
+
+quartz_status quartz_mxfp4_linear_kernel(int64_t M, int64_t N, int64_t K, int32_t* kernel)
+{
+    if (M <= 0 || N <= 0)
+        return QUARTZ_ERR_SHAPE;
+    const quartz_status st = mx_linear_checks(M, N, K, N, QUARTZ_EPI_NONE);
+    if (st != QUARTZ_OK)
+        return st;
+    if (!kernel)
+        return QUARTZ_ERR_NULL;
+    const MxShape s = mxfp4_shape(M, N, K);
+    const int unit = s.tiled ? 64 : 16;
+    kernel[0] = s.tiled ? QUARTZ_MX_TILED : QUARTZ_MX_DIRECT;
+    kernel[1] = unit * s.tm;
+    kernel[2] = unit * s.tn;
+    kernel[3] = mxfp4_fuses(M, K);
+    return QUARTZ_OK;
 }
 
 quartz_status quartz_rotary_frequencies(int64_t rot, double base, int32_t scaling, double factor, double low,

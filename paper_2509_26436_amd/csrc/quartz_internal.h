@@ -268,7 +268,7 @@ hipError_t launch_mxfp4_quantize(const uint16_t* x, int64_t M, int64_t K, int64_
 hipError_t launch_mxfp4_dequantize(const uint8_t* codes, const uint8_t* scales, int64_t M, int64_t K,
                                    uint16_t* y, int64_t ldy, hipStream_t stream);
 // y [M][ldy] = act(A W^T + bias); A either in MXFP4 (x_codes, x_scales) or, if
-// mxfp4_fuses(M), in bf16 (x [M][ldx], quantized within the kernel).
+// mxfp4_fuses(M, K), in bf16 (x [M][ldx], quantized within the kernel).
 struct MxLinear {
     const uint16_t* x;
     int64_t ldx;
@@ -281,7 +281,14 @@ struct MxLinear {
     int64_t M, N, K, ldy;
     bool gelu;
 };
-bool mxfp4_fuses(int64_t M);
+bool mxfp4_fuses(int64_t M, int64_t K);
+// Tile of the kernel that a call on MXFP4 activations launches: 16 tm tokens x
+// 16 tn columns in direct blocks, 64 tm x 64 tn in tiled ones.  Host only.
+struct MxShape {
+    bool tiled;
+    int tm, tn;
+};
+MxShape mxfp4_shape(int64_t M, int64_t N, int64_t K);
 hipError_t launch_mxfp4_linear(const MxLinear& a, hipStream_t stream);
 
 // ------------------------------------------------------------ decoding

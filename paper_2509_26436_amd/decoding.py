@@ -23,6 +23,7 @@ _SIGNATURES = {
     "quartz_mxfp4_linear": ([P] * 6 + [I64] * 4 + [I32, P], I32),
     "quartz_mxfp4_linear_workspace_bytes": ([I64, I64], SZ),
     "quartz_mxfp4_linear_bf16": ([P, I64, P, P, P, P, I64, I64, I64, I64, I32, P, SZ, P], I32),
+    "quartz_mxfp4_linear_kernel": ([I64, I64, I64, P], I32),
     "quartz_rotary_frequencies": ([I64, F64, I32, F64, F64, F64, F64, P], I32),
     "quartz_rotary": ([P, P] + [I64] * 8 + [P, P, I32, I32, F32, P], I32),
     "quartz_paged_append": ([P, P] + [I64] * 7 + [P, P, P, I64, I32, F32, P, P, I32, F32, F32, I64, I64,
@@ -64,6 +65,10 @@ def quartz_mxfp4_linear_bf16(x, ldx, w_codes, w_scales, bias, y, M, N, K, ldy, e
                              workspace_bytes, stream) -> int:
     return _q.load().quartz_mxfp4_linear_bf16(x, ldx, w_codes, w_scales, bias, y, M, N, K, ldy,
                                               epilogue, workspace, workspace_bytes, stream)
+
+
+def quartz_mxfp4_linear_kernel(M, N, K, kernel) -> int:
+    return _q.load().quartz_mxfp4_linear_kernel(M, N, K, kernel)
 
 
 def quartz_rotary_frequencies(rot, base, scaling, factor, low, high, original, freqs) -> int:
@@ -191,6 +196,20 @@ def mxfp4_linear(x, w: MxTensor, bias=None, epilogue: int = 0, out=None, stream=
         return _native().linear_mx(x.codes, x.scales, x.rows, x.K, w.codes, w.scales, w.rows, w.K, bias,
                                    epilogue, out)
     return _native().linear_bf16(x, w.codes, w.scales, w.rows, w.K, bias, epilogue, out, workspace)
+
+
+MX_KERNELS = ("direct", "tiled")
+
+
+def mxfp4_linear_kernel(M: int, N: int, K: int) -> dict:
+    """The kernel that ``mxfp4_linear`` launches for these sizes (quartz_mxfp4_linear_kernel, host
+    only): kernel (one of MX_KERNELS), tile rows (tokens) and columns, and whether bf16 activations
+    are quantized within it."""
+    out = (ctypes.c_int32 * 4)()
+    status = quartz_mxfp4_linear_kernel(M, N, K, ctypes.addressof(out))
+    if status:
+        raise _q.QuartzError(status, "quartz_mxfp4_linear_kernel")
+    return {"kernel": MX_KERNELS[out[0]], "rows": out[1], "cols": out[2], "fused": bool(out[3])}
 
 
 def rotary_frequencies(rot: int, base: float = 10000.0, scaling: str = "linear", factor: float = 1.0,

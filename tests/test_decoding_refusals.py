@@ -60,6 +60,19 @@ def test_mxfp4_linear_from_bf16():
     assert call(M=0, size=0, work=None) == call(N=0, ldy=0) == OK
 
 
+def test_mxfp4_linear_kernel():
+    """Every kernel is some size's, and which: direct blocks for few tokens, tiles for many."""
+    for M, N, K, kernel, rows, cols, fused in (
+            (1, 4096, 4096, "direct", 16, 16, True), (8, 4096, 4096, "direct", 16, 16, True),
+            (8, 4096, 4160, "direct", 16, 16, False), (9, 4096, 64, "direct", 16, 16, False),
+            (64, 4096, 4096, "direct", 32, 32, False), (256, 4096, 4096, "direct", 64, 64, False),
+            (1024, 4096, 4096, "tiled", 128, 128, False), (4096, 4096, 4096, "tiled", 256, 256, False),
+            (4608, 8192, 8192, "tiled", 192, 256, False), (8192, 4608, 8192, "tiled", 256, 192, False)):
+        assert q.mxfp4_linear_kernel(M, N, K) == {"kernel": kernel, "rows": rows, "cols": cols, "fused": fused}
+    assert q.quartz_mxfp4_linear_kernel(0, 8, 64, A) == q.quartz_mxfp4_linear_kernel(8, 8, 96, A) == ESHAPE
+    assert q.quartz_mxfp4_linear_kernel(8, 8, 64, None) == ENULL
+
+
 def test_rotary():
     def call(x=A, y=1 << 20, T=4, H=2, d=64, rot=64, xt=128, xh=64, yt=128, yh=64, pos=A, f=A, layout=0,
              inverse=0, magnitude=1.0):

@@ -123,10 +123,18 @@ def test_linear(M, N, K, act, with_bias):
         assert (out[:, N:] == 5.0).all()
 
 
-@pytest.mark.parametrize("M,N,K", [(2048, 2048, 256), (1999, 2100, 320), (2304, 4100, 1152), (4000, 1100, 64)])
-def test_linear_large(M, N, K):
-    """Sizes of the large tiles, ragged and with a last step of K that is not whole; sampled rows."""
+@pytest.mark.parametrize("M,N,K,tile", [(2048, 2048, 256, (128, 128)), (1999, 2100, 320, (128, 128)),
+                                        (4090, 4093, 64, (128, 128)), (4000, 1100, 2112, (128, 128)),
+                                        (4090, 4093, 1216, (256, 256)), (4090, 4093, 2048, (256, 256)),
+                                        (2304, 4100, 1152, (192, 256)), (4600, 8190, 448, (192, 256)),
+                                        (8190, 4599, 832, (256, 192)),
+                                        (200, 4000, 2112, (32, 32)), (300, 3001, 4096, (64, 64))])
+def test_linear_large(M, N, K, tile):
+    """Sizes of the larger tiles, ragged, with K of one step, shorter than the ring of stages, and with
+    a last stage of one step; sampled rows."""
     import paper_2509_26436_amd as q
+    kernel = q.mxfp4_linear_kernel(M, N, K)
+    assert (kernel["rows"], kernel["cols"]) == tile
     print(f"mxfp4 large {M} x {N} x {K}", flush=True)
     rng = _rng(4, M, N, K)
     x = _tokens(rng, M, K, 1.0)
