@@ -6,6 +6,7 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <ATen/MemoryOverlap.h>
 #include <c10/hip/HIPGuard.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
@@ -38,6 +39,13 @@ int64_t integer(PyObject* o)
     return v;
 }
 
+int32_t small(PyObject* o, const char* what)
+{
+    const int64_t v = integer(o);
+    NEED(v >= INT32_MIN && v <= INT32_MAX, what, " is out of range");
+    return (int32_t)v;
+}
+
 double real(PyObject* o)
 {
     const double v = PyFloat_AsDouble(o);
@@ -56,6 +64,30 @@ int32_t layout_of(PyObject* o)
     }
     NEED(false, "layout must be \"half\" or \"interleaved\"");
     return 0;
+}
+
+// strides count where more than one element is reached
+bool strided(const Tensor& t, int64_t dim) { return t.size(dim) > 1 && t.numel() > 0; }
+bool unit(const Tensor& t, int64_t dim) { return !strided(t, dim) || t.stride(dim) == 1; }
+
+// an output whose elements are distinct, and (where that can be seen) none of them an input's
+template <typename... T>
+void fresh(const Tensor& out, const T&... inputs)
+{
+    if (!out.defined())
+        return;
+    NEED(at::has_internal_overlap(out) != at::MemOverlap::Yes, "out must not hold one element twice");
+    [[maybe_unused]] auto check = [&](const Tensor& t) {
+        const at::MemOverlapStatus shared = t.defined() ? at::get_overlap_status(out, t) : at::MemOverlapStatus::No;
+        NEED(shared != at::MemOverlapStatus::Full && shared != at::MemOverlapStatus::Partial,
+             "out must not share memory with an input");
+    };
+    (check(inputs), ...);
+}
+
+bool in_place(const Tensor& out, const Tensor& x)
+{
+    return out.defined() && out.data_ptr() == x.data_ptr() && out.sizes() == x.sizes() && out.strides() == x.strides();
 }
 
 void* address(const Tensor& t) { return t.defined() ? t.data_ptr() : nullptr; }
@@ -97,9 +129,9 @@ void launch(const char* name, const Tensor& on, F&& call)
 // leading dimension of a bf16 matrix with unit column stride
 int64_t rows_of(const Tensor& t, const char* what)
 {
-    NEED(t.scalar_type() == at::kBFloat16 && t.dim() == 2 && (t.stride(1) == 1 || t.size(1) <= 1), what,
+    NEED(t.scalar_type() == at::kBFloat16 && t.dim() == 2 && unit(t, 1), what,
          " must be a 2-D bf16 tensor with unit column stride");
-    return t.size(0) > 1 ? t.stride(0) : (t.size(1) + 7) / 8 * 8;
+    return strided(t, 0) ? t.stride(0) : (t.size(1) + 7) / 8 * 8;
 }
 
 struct Mx {
@@ -169,6 +201,8 @@ PyObject* quantize_into(PyObject*, PyObject* const* a, Py_ssize_t n)
     const int64_t ldx = rows_of(x, "x"), M = x.size(0), K = x.size(1);
     const Mx t = mx_of(a[1], a[2], a[3], a[4]);
     NEED(t.rows == M && t.K == K, "out must have x's rows and K");
+    fresh(t.codes, x, t.scales);
+    fresh(t.scales, x);
     same_device(x, t.codes);
     launch("quartz_mxfp4_quantize", x, [&](hipStream_t s) {
         return quartz_mxfp4_quantize(x.data_ptr(), M, K, ldx, static_cast<uint8_t*>(t.codes.data_ptr()),
@@ -185,6 +219,7 @@ PyObject* dequantize(PyObject*, PyObject* const* a, Py_ssize_t n)
     ARGUMENTS(5)
     const Mx t = mx_of(a[0], a[1], a[2], a[3]);
     Tensor out = optional(a[4], "out");
+    fresh(out, t.codes, t.scales);
     same_device(t.codes, out);
     if (!out.defined())
         out = at::empty({t.rows, t.K}, t.codes.options().dtype(at::kBFloat16));
@@ -200,8 +235,7 @@ PyObject* dequantize(PyObject*, PyObject* const* a, Py_ssize_t n)
 // checks bias and out of a layer [M, N]; returns ldy
 int64_t layer_out(const Tensor& on, int64_t M, int64_t N, const Tensor& bias, Tensor& out)
 {
-    NEED(!bias.defined() || (bias.scalar_type() == at::kBFloat16 && bias.dim() == 1 && bias.size(0) == N &&
-                             (bias.stride(0) == 1 || N <= 1)),
+    NEED(!bias.defined() || (bias.scalar_type() == at::kBFloat16 && bias.dim() == 1 && bias.size(0) == N && unit(bias, 0)),
          "bias must be bf16 [N], contiguous");
     if (!out.defined()) {
         out = at::empty({M, N}, on.options().dtype(at::kBFloat16).requires_grad(false));
@@ -219,9 +253,10 @@ PyObject* linear_mx(PyObject*, PyObject* const* a, Py_ssize_t n)
     ARGUMENTS(11)
     const Mx x = mx_of(a[0], a[1], a[2], a[3]), w = mx_of(a[4], a[5], a[6], a[7]);
     const Tensor bias = optional(a[8], "bias");
-    const int32_t epilogue = (int32_t)integer(a[9]);
+    const int32_t epilogue = small(a[9], "epilogue");
     Tensor out = optional(a[10], "out");
     NEED(x.K == w.K, "K mismatch between activations and weights");
+    fresh(out, x.codes, x.scales, w.codes, w.scales, bias);
     same_device(w.codes, x.codes, bias, out);
     const int64_t ldy = layer_out(w.codes, x.rows, w.rows, bias, out);
     launch("quartz_mxfp4_linear", out, [&](hipStream_t s) {
@@ -252,10 +287,11 @@ PyObject* linear_bf16(PyObject*, PyObject* const* a, Py_ssize_t n)
     const Tensor& x = tensor(a[0], "x");
     const Mx w = mx_of(a[1], a[2], a[3], a[4]);
     const Tensor bias = optional(a[5], "bias");
-    const int32_t epilogue = (int32_t)integer(a[6]);
+    const int32_t epilogue = small(a[6], "epilogue");
     Tensor out = optional(a[7], "out"), workspace = optional(a[8], "workspace");
     const int64_t ldx = rows_of(x, "x"), M = x.size(0);
     NEED(x.size(1) == w.K, "K mismatch between activations and weights");
+    fresh(out, x, w.codes, w.scales, bias, workspace);
     same_device(x, w.codes, bias, out, workspace);
     const int64_t ldy = layer_out(x, M, w.rows, bias, out);
     const size_t size = workspace_of(workspace, quartz_mxfp4_linear_workspace_bytes(M, w.K), x);
@@ -269,13 +305,13 @@ PyObject* linear_bf16(PyObject*, PyObject* const* a, Py_ssize_t n)
 
 void heads_of(const Tensor& t, const char* what)
 {
-    NEED(t.scalar_type() == at::kBFloat16 && t.dim() == 3 && (t.stride(2) == 1 || t.size(2) <= 1), what,
+    NEED(t.scalar_type() == at::kBFloat16 && t.dim() == 3 && unit(t, 2), what,
          " must be a bf16 [tokens, heads, d] tensor with unit stride along d");
 }
 
 const int32_t* int32_of(const Tensor& t, int64_t count, const char* what)
 {
-    NEED(t.scalar_type() == at::kInt && t.dim() == 1 && t.size(0) == count && (t.stride(0) == 1 || count <= 1), what,
+    NEED(t.scalar_type() == at::kInt && t.dim() == 1 && t.size(0) == count && unit(t, 0), what,
          " must be a contiguous int32 tensor of ", count);
     return static_cast<const int32_t*>(t.data_ptr());
 }
@@ -303,6 +339,7 @@ PyObject* rotary(PyObject*, PyObject* const* a, Py_ssize_t n)
         throw python_error();
     const float magnitude = (float)real(a[5]);
     Tensor out = optional(a[6], "out");
+    fresh(out, in_place(out, x) ? Tensor() : x, positions, freqs);
     same_device(x, positions, freqs, out);
     if (!out.defined())
         out = at::empty_like(x, x.options().requires_grad(false));
@@ -339,9 +376,9 @@ Cache cache_of(PyObject* k, PyObject* v, PyObject* table, PyObject* k_scale, PyO
     NEED((type == at::kBFloat16 || type == at::kFloat8_e4m3fn) && c.v.scalar_type() == type,
          "k and v must both be bf16 or both float8_e4m3fn");
     NEED(c.k.dim() == 4 && c.k.sizes() == c.v.sizes(), "k and v must be [pages, heads, page_size, d], both alike");
-    NEED(page_contiguous(c.k) && page_contiguous(c.v) && (c.k.size(0) <= 1 || c.k.stride(0) == c.v.stride(0)),
+    NEED(page_contiguous(c.k) && page_contiguous(c.v) && (!strided(c.k, 0) || c.k.stride(0) == c.v.stride(0)),
          "a page must be contiguous, and k and v must have one page stride");
-    NEED(c.table.scalar_type() == at::kInt && c.table.dim() == 2 && (c.table.stride(1) == 1 || c.table.size(1) <= 1),
+    NEED(c.table.scalar_type() == at::kInt && c.table.dim() == 2 && unit(c.table, 1),
          "table must be an int32 [sequences, pages] tensor with unit column stride");
     NEED(c.k.device() == c.v.device() && c.k.device() == c.table.device(), "k, v and table must be on one device");
     c.type = type == at::kBFloat16 ? QUARTZ_CACHE_BF16 : QUARTZ_CACHE_E4M3;
@@ -349,12 +386,12 @@ Cache cache_of(PyObject* k, PyObject* v, PyObject* table, PyObject* k_scale, PyO
     c.heads = c.k.size(1);
     c.page = c.k.size(2);
     c.d = c.k.size(3);
-    c.stride = c.pages > 1 ? c.k.stride(0) : c.heads * c.page * c.d;
+    c.stride = strided(c.k, 0) ? c.k.stride(0) : c.heads * c.page * c.d;
     return c;
 }
 
 const int32_t* table_at(const Cache& c) { return static_cast<const int32_t*>(c.table.data_ptr()); }
-int64_t table_stride(const Cache& c) { return c.table.size(0) > 1 ? c.table.stride(0) : c.table.size(1); }
+int64_t table_stride(const Cache& c) { return strided(c.table, 0) ? c.table.stride(0) : c.table.size(1); }
 
 // (k, v, table, k_scale, v_scale)
 PyObject* check_cache(PyObject*, PyObject* const* a, Py_ssize_t n)
@@ -411,7 +448,9 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n)
     const int32_t* len = int32_of(lengths, sequences, "lengths");
     const float scale = a[7] == Py_None ? (float)(1.0 / std::sqrt((double)d)) : (float)real(a[7]);
     Tensor out = optional(a[9], "out"), workspace = optional(a[10], "workspace");
+    fresh(out, q, c.k, c.v, c.table, lengths, workspace);
     same_device(c.k, q, lengths, out, workspace);
+    const c10::hip::OptionalHIPGuard guard(q.device().index());    // the workspace is sized for its compute units
     if (!out.defined())
         out = at::empty({sequences, heads, d}, q.options().requires_grad(false));
     heads_of(out, "out");

@@ -268,9 +268,10 @@ def paged_append(cache: PagedCache, k, v, positions, sequences=None, freqs=None,
 def paged_attention_workspace(sequences: int, heads: int, cache: PagedCache, window: int = 0):
     """Workspace of ``paged_attention`` for these sizes, or None where it needs none."""
     _, kv_heads, page, d = cache.k.shape
-    n = quartz_paged_attention_workspace_bytes(sequences, heads, kv_heads, d, page, cache.table.shape[1],
-                                               window)
     torch = _q._torch()
+    with torch.cuda.device(cache.k.device):      # sized for its compute units
+        n = quartz_paged_attention_workspace_bytes(sequences, heads, kv_heads, d, page, cache.table.shape[1],
+                                                   window)
     return torch.empty((n,), dtype=torch.uint8, device=cache.k.device) if n else None
 
 

@@ -218,3 +218,48 @@ def test_helpers_refuse_tensors():
             print("not refused:", i)
     with pytest.raises(q.QuartzError):
         q.rotary_frequencies(64, factor=0.5, device="cpu")
+
+
+def test_helpers_refuse_shared_memory():
+    """Outputs that hold an element twice, or that are an input's memory; epilogues past 32 bits."""
+    import torch
+    x = torch.zeros((8, 128), dtype=torch.bfloat16)
+    codes, scales = torch.zeros((4, 8, 16), dtype=torch.uint8), torch.zeros((1, 8, 4), dtype=torch.uint8)
+    w, other = q.MxTensor(codes, scales, 8, 128), q.MxTensor(codes.clone(), scales.clone(), 8, 128)
+    heads = torch.zeros((4, 2, 128), dtype=torch.bfloat16)
+    pos, f = torch.zeros(4, dtype=torch.int32), q.rotary_frequencies(128, device="cpu")
+    k = torch.zeros((3, 2, 16, 128), dtype=torch.bfloat16)
+    cache = q.PagedCache(k, k.clone(), torch.zeros((4, 2), dtype=torch.int32))
+    x16 = codes.view(-1).view(torch.bfloat16)
+    wrong = [
+        (lambda: q.mxfp4_linear(x, w, out=x), "share"), (lambda: q.mxfp4_linear(other, w, out=x[:1].expand(8, 128)), "twice"),
+        (lambda: q.mxfp4_linear(x, w, epilogue=2 ** 32), "range"), (lambda: q.mxfp4_linear(other, w, epilogue=2 ** 32), "range"),
+        (lambda: q.mxfp4_linear(other, w, out=x16[:64].view(8, 8)), "share"),
+        (lambda: q.mxfp4_quantize(x16.view(2, 128), out=q.MxTensor(codes.view(-1)[:128].view(4, 2, 16), scales[:, :2].clone(), 2, 128)), "share"),
+        (lambda: q.mxfp4_dequantize(q.MxTensor(codes[:, :2].clone(), scales[:, :2], 2, 128), out=torch.zeros(1, dtype=torch.bfloat16).expand(2, 128)), "twice|stride"),
+        (lambda: q.rotary(heads, pos, f, out=heads[:1].expand(4, 2, 128)), "twice"),
+        (lambda: q.rotary(heads[:1].expand(4, 2, 128), pos, f, out=heads[:1].expand(4, 2, 128)), "twice"),
+        (lambda: q.rotary(heads.view(-1)[:512].view(2, 2, 128), pos[:2], f, out=heads.view(-1)[8:520].view(2, 2, 128)), "share"),
+        (lambda: q.paged_attention(heads, cache, pos, out=heads), "share"),
+        (lambda: q.paged_attention(heads, cache, pos, out=torch.zeros_like(heads[:, :1]).expand(4, 2, 128)), "twice"),
+        (lambda: q.paged_attention(heads, cache, pos, out=k[0].view(-1)[:1024].view(4, 2, 128)), "share")]
+    for i, (call, why) in enumerate(wrong):
+        print("refused?", i)
+        with pytest.raises(ValueError, match=why):
+            call()
+
+
+def test_helpers_take_empty_tensors_of_any_strides():
+    """Strides of tensors without elements say nothing: the refusal that is left is the missing GPU."""
+    import torch
+    none = torch.empty_strided((0, 8), (0, 0), dtype=torch.int32)
+    k = torch.zeros((3, 2, 16, 128), dtype=torch.bfloat16)
+    cache = q.PagedCache(k, k.clone(), none)
+    q.PagedCache(k, k.clone(), torch.empty_strided((4, 0), (0, 0), dtype=torch.int32))
+    heads = torch.empty_strided((0, 2, 128), (0, 0, 0), dtype=torch.bfloat16)
+    pos, f = torch.zeros(0, dtype=torch.int32), q.rotary_frequencies(128, device="cpu")
+    for call in (lambda: q.mxfp4_quantize(torch.empty_strided((0, 128), (0, 0), dtype=torch.bfloat16)),
+                 lambda: q.rotary(heads, pos, f), lambda: q.paged_append(cache, heads, heads, pos),
+                 lambda: q.paged_attention(heads, cache, pos)):
+        with pytest.raises(ValueError, match="on a GPU"):
+            call()
