@@ -672,11 +672,10 @@ quartz_status quartz_rotary(const void* x_bf16, void* y_bf16, int64_t tokens, in
  *              for q, of 4 for o (whose pointer needs 8-byte alignment).
  *   table      row b belongs to sequence b (rows = sequences).
  *   workspace  quartz_paged_attention_workspace_bytes of the same sizes (0: none
- *              needed), any contents.  Calls that share one must not overlap in
- *              time.
- * The work is split by the table's width, not by the lengths (which the host
- * does not read): a call may be captured into a graph and replayed with other
- * lengths, pages and tokens.
+ *              needed) on the current device, any contents.  Calls that share one
+ *              must not overlap in time.
+ * The host reads no lengths (the kernels share the work by them): a call may be
+ * captured into a graph and replayed with other lengths, pages and tokens.
  */
 enum { QUARTZ_CACHE_BF16 = 0, QUARTZ_CACHE_E4M3 = 1 };
 

@@ -1,6 +1,7 @@
 // C-ABI entry points of the decoding step: MXFP4 quantization and linear layer,
 // rotary positions, paged cache and attention.  Host-side validation, then the
 // launch on the caller's stream; include/quartz.h has the contract of each.
+#include <algorithm>
 #include <cfloat>
 #include <cmath>
 
@@ -304,33 +305,33 @@ quartz_status quartz_paged_append(const void* k_bf16, const void* v_bf16, int64_
     return from_hip(launch_paged_append(a, stream));
 }
 
-// sizes of an attention call, and how its keys are split
+// sizes of an attention call; `longest`: keys of a sequence at most
 static quartz_status attention_checks(int64_t sequences, int64_t heads, int64_t kv_heads, int64_t d,
-                                      int64_t page_size, int64_t table_pages, int64_t window, PagedSplit& split)
+                                      int64_t page_size, int64_t table_pages, int64_t window, int64_t& longest)
 {
     if ((d != 64 && d != 128 && d != 256) || page_size < 8 || page_size > 4096 ||
         (page_size & (page_size - 1)) != 0)
         return QUARTZ_ERR_UNSUPPORTED;
-    if (sequences < 0 || sequences > kMaxBlocks256 || kv_heads <= 0 || heads < kv_heads || heads > kMaxK ||
-        heads % kv_heads != 0 || table_pages < 0 || table_pages > kMaxPositions / page_size || window < 0)
+    if (sequences < 0 || sequences > kMaxBlocks512 || kv_heads <= 0 || heads < kv_heads || heads > kMaxK ||
+        heads % kv_heads != 0 || table_pages < 0 || table_pages > kMaxPositions / page_size || window < 0 ||
+        !product_ok(sequences, heads, kMaxBlocks512))
         return QUARTZ_ERR_SHAPE;
-    int64_t longest = table_pages * page_size;
+    longest = table_pages * page_size;
     if (window > 0 && window < longest)
         longest = window;
-    split = paged_split(sequences, heads, kv_heads, d, longest);
-    if (!product_ok(sequences * heads, split.splits, kMaxBlocks256))
-        return QUARTZ_ERR_SHAPE;
     return QUARTZ_OK;
 }
 
 size_t quartz_paged_attention_workspace_bytes(int64_t sequences, int64_t heads, int64_t kv_heads, int64_t d,
                                               int64_t page_size, int64_t table_pages, int64_t window)
 {
-    PagedSplit split;
-    if (attention_checks(sequences, heads, kv_heads, d, page_size, table_pages, window, split) != QUARTZ_OK ||
+    int64_t longest = 0;
+    if (attention_checks(sequences, heads, kv_heads, d, page_size, table_pages, window, longest) != QUARTZ_OK ||
         sequences == 0)
         return 0;
-    return paged_attention_bytes(sequences, heads, d, split);
+    // enough for either cache type
+    return paged_attention_bytes(d, std::max(paged_blocks(sequences, heads, kv_heads, d, false, longest),
+                                             paged_blocks(sequences, heads, kv_heads, d, true, longest)));
 }
 
 quartz_status quartz_paged_attention(const void* q_bf16, void* o_bf16, int64_t sequences, int64_t heads,
@@ -344,8 +345,8 @@ quartz_status quartz_paged_attention(const void* q_bf16, void* o_bf16, int64_t s
 {
     if (!std::isfinite(scale))
         return QUARTZ_ERR_UNSUPPORTED;
-    PagedSplit split;
-    quartz_status st = attention_checks(sequences, heads, kv_heads, d, page_size, table_pages, window, split);
+    int64_t longest = 0;
+    quartz_status st = attention_checks(sequences, heads, kv_heads, d, page_size, table_pages, window, longest);
     if (st != QUARTZ_OK)
         return st;
     if (!stride_ok(q_token) || !stride_ok(q_head) || !stride_ok(o_token) || !stride_ok(o_head))
@@ -362,7 +363,8 @@ quartz_status quartz_paged_attention(const void* q_bf16, void* o_bf16, int64_t s
     if (!aligned16(q_bf16) || !aligned(o_bf16, 8) || !aligned(lengths, 4) || !aligned16(workspace) ||
         ((q_token | q_head) & 7) != 0 || ((o_token | o_head) & 3) != 0)
         return QUARTZ_ERR_ALIGN;
-    const size_t need = paged_attention_bytes(sequences, heads, d, split);
+    const int blocks = paged_blocks(sequences, heads, kv_heads, d, a.cache.fp8, longest);
+    const size_t need = paged_attention_bytes(d, blocks);
     if (need > 0 && (!workspace || workspace_bytes < need))
         return QUARTZ_ERR_WORKSPACE;
     a.q = static_cast<const uint16_t*>(q_bf16);
@@ -375,8 +377,7 @@ quartz_status quartz_paged_attention(const void* q_bf16, void* o_bf16, int64_t s
     a.lengths = lengths;
     a.scale = scale;
     a.window = (int32_t)(window < kMaxPositions ? window : kMaxPositions);
-    a.split_keys = split.keys;
-    a.splits = split.splits;
+    a.shared = blocks;
     a.workspace = static_cast<float*>(workspace);
     return from_hip(launch_paged_attention(a, stream));
 }

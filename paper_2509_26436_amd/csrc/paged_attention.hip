@@ -5,24 +5,33 @@
 // and values: each is read once and used by the `group` query heads that share
 // it, up to 16 of them as the columns of one matrix tile.
 //
-// A block takes a run of split_keys keys of one (sequence, cache head); its
-// four waves take 32 keys at a time.  No key or value passes through shared
-// memory, because the matrix instructions' rows may be any keys and channels:
+// No key or value passes through shared memory, because the matrix
+// instructions' rows may be any keys and channels:
 //   S^T = K Q^T: row 4 a + i of tile t is key 8 a + 4 t + i, so that the scores
 //     a lane gets (one query, rows 4 g .. 4 g + 3 of two tiles) are keys 8 g ..
 //     8 g + 7: exactly the 8 keys of its share of P^T in the next product;
-//   O^T = V^T P^T: lane (m, g) reads channels (D/16) m .. + D/16 of keys 8 g ..
-//     8 g + 7, whole rows of V over the 16 lanes, and turns the 8 x D/16 block
-//     in registers; row m of tile t is channel (D/16) m + t, so that at the end
-//     a lane holds D/16 neighbouring channels of its query.
+//   O^T = V^T P^T: lane (m, g) reads a run of channels of keys 8 g .. 8 g + 7,
+//     whole rows of V over the 16 lanes m, and turns the block of 8 keys x run in
+//     registers; row m of tile t is channel t of lane m's run, so that at the end
+//     a lane holds neighbouring channels of its query.
 // The softmax runs over the pass with a running maximum and sum in fp32 (base-2
 // exponentials).  P is rounded to bf16 for the product, with a relative error of
-// up to 2^-9 a weight as for the output itself, and the sum is that of the
+// up to 2^-8 a weight as for the output itself, and the sum is that of the
 // rounded weights (a row of ones beside V), so that weights add up to one.
 // e4m3 keys and values are expanded to bf16, exactly, after the load; their
 // scales go into the softmax scale and the output.
-// Sequences longer than split_keys leave (maximum, sum, O) of every run in the
-// workspace, and a second kernel joins them.
+//
+// The work of a call is a list of units, 128 keys of one (sequence, cache head,
+// 16 queries) each, sequence after sequence, that the blocks share in equal
+// runs: a block passes over its units with four waves of 32 keys, the next 32
+// on their way while it computes, and whenever it leaves a sequence's head its
+// waves' sums meet in shared memory.  A head that lies within one block's run is
+// finished there; of the others each block leaves (maximum, sum, O) in the
+// workspace, at most two such parts a block, and a second kernel joins them.
+// Where the table is narrow every head is one block's, and there is no second
+// kernel.
+#include <algorithm>
+
 #include "quartz_internal.h"
 
 namespace quartz {
@@ -34,11 +43,34 @@ typedef float f2 __attribute__((ext_vector_type(2)));
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef uint32_t v4u __attribute__((ext_vector_type(4)));
 
-constexpr int kWaves = 4;
-constexpr int kKeys = 32;                        // keys of a wave's step
-constexpr int kMostSplitKeys = 4096;
-constexpr int kLeastPage = 8;
+constexpr int kKeys = 32;                        // keys of a matrix tile
+// Tiles of a wave's step: as many as make its loads 16 KB (8 KB for e4m3 of 64
+// channels), which keeps the memory busy with the waves that fit.
+constexpr int step_tiles(int d, bool fp8) { return d == 64 || (d == 128 && fp8) ? 2 : 1; }
+// keys of a unit of work: a step of four waves
+constexpr int unit_keys(int d, bool fp8) { return 4 * kKeys * step_tiles(d, fp8); }
 constexpr float kNoScore = -3.0e38f;             // a maximum below every score that counts
+
+// N words that are read once (16-byte loads around the caches' replacement
+// reach 7.1 TB/s where ordinary ones reach 6.2)
+template <int N>
+__device__ __forceinline__ auto once(const uint8_t* p)
+{
+    typedef uint32_t words __attribute__((ext_vector_type(N)));
+    return __builtin_nontemporal_load(reinterpret_cast<const words*>(p));
+}
+
+// 16 bytes of a key's row, whose 64-byte stretch an instruction reads.  Once is
+// better for 128 channels (8 heads of 262143 keys: 161 us, else 164) and worse
+// for 64 and 256 (32.1 against 29.5 us, 36.8 against 33.7).
+template <bool ONCE>
+__device__ __forceinline__ v4u load(const uint8_t* p)
+{
+    if constexpr (ONCE)
+        return once<4>(p);
+    else
+        return *reinterpret_cast<const v4u*>(p);
+}
 
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b)
 {
@@ -66,135 +98,272 @@ __device__ __forceinline__ v4f mfma(v4u a, v4u b, v4f c)
                                                    0, 0);
 }
 
-// the keys of a sequence that count: [first, n)
+// the keys of a sequence that count, [first, n), and their units from `from` on
 struct KeyRange {
-    int n, first;
+    int n, first, from, units;
 };
-__device__ __forceinline__ KeyRange key_range(const PagedAttention& a, int64_t b)
+__device__ __forceinline__ KeyRange key_range(const PagedAttention& a, int64_t b, int unit)
 {
     KeyRange r;
     r.n = min(max(a.lengths[b], 0), a.cache.table_pages << a.cache.page_shift);
     r.first = a.window > 0 ? max(0, r.n - a.window) : 0;
+    r.from = r.first & ~(kKeys - 1);
+    r.units = (r.n - r.from + unit - 1) / unit;
     return r;
 }
 
-template <int D, bool FP8>
-__global__ __launch_bounds__(64 * kWaves) void paged_attention_kernel(const PagedAttention a, uint32_t tiles)
+// units [first, first + count) of `total` that block i of `blocks` takes
+struct Share {
+    int64_t first, count;
+};
+__device__ __forceinline__ Share share_of(int64_t total, int64_t blocks, int64_t i)
 {
+    const int64_t each = total / blocks, more = total - each * blocks;
+    return {i * each + min(i, more), each + (i < more ? 1 : 0)};
+}
+// the block that takes unit u
+__device__ __forceinline__ int64_t block_of(int64_t total, int64_t blocks, int64_t u)
+{
+    const int64_t each = total / blocks, more = total - each * blocks, border = more * (each + 1);
+    return u < border ? u / (each + 1) : more + (u - border) / each;
+}
+
+// What the blocks of a shared call leave: two parts each of 16 queries (sums of
+// their first and their last head), a maximum and a sum a query, and, of a block
+// in which a head begins that others go on with, where the join finds it.
+struct Part {
+    int64_t b;
+    int head0, queries, slot, blocks;            // blocks that have a part, this one first; 0: nothing to join
+};
+__device__ __forceinline__ float* parts_o(const PagedAttention& a) { return a.workspace; }
+__device__ __forceinline__ f2* parts_ml(const PagedAttention& a, int d)
+{
+    return reinterpret_cast<f2*>(a.workspace + (int64_t)a.shared * 32 * d);
+}
+__device__ __forceinline__ Part* parts_of(const PagedAttention& a, int d)
+{
+    return reinterpret_cast<Part*>(a.workspace + (int64_t)a.shared * 32 * (d + 2));
+}
+
+// the waves' shared-memory accesses are done; loads stay on their way
+__device__ __forceinline__ void meet() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+// the head that a block works on: sequence b, cache head and queries `part`,
+// units [unit, unit + count) of it
+struct Head {
+    int64_t b;
+    int part, unit, count;
+    KeyRange range;
+};
+
+// waves a block may use, and blocks of four waves that fit a compute unit
+constexpr int fits(int d, bool fp8) { return d == 64 ? 3 : d == 128 ? (fp8 ? 2 : 3) : 1; }
+
+// SHARED: a block takes a run of units; otherwise a head.
+template <int D, bool FP8, int WAVES, bool SHARED>
+__global__ __launch_bounds__(64 * WAVES, SHARED ? fits(D, FP8) : 1) void paged_attention_kernel(
+    const PagedAttention a, int tiles)
+{
+    constexpr int kWaves = WAVES, kThreads = 64 * kWaves;
+    constexpr int kR = step_tiles(D, FP8), kStep = kKeys * kR, kPass = kStep * kWaves, kUnit = unit_keys(D, FP8);
     constexpr int kSteps = D / 32;               // matrix steps over the channels
     constexpr int kTiles = D / 16;               // row tiles of O^T
+    constexpr int kRun = FP8 || D < 256 ? kTiles : 8;        // channels of a lane's load of V: at most 16 bytes
     constexpr int kRow = D + 4;
-    __shared__ float part[kWaves][16][kRow];
+    constexpr int kBytes = FP8 ? 1 : 2;
+    __shared__ float part_o[kWaves][16][kRow];
     __shared__ float part_m[kWaves][16], part_l[kWaves][16];
-    __shared__ int32_t ids[kMostSplitKeys / kLeastPage + 1];
+    __shared__ uint32_t sums[kWaves];
+    __shared__ int64_t found[2];
 
     const PagedCacheView& c = a.cache;
     const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const uint32_t split = blockIdx.x % (uint32_t)a.splits, rest = blockIdx.x / (uint32_t)a.splits;
-    const uint32_t part_of = rest % (c.heads * tiles);
-    const int64_t b = rest / (c.heads * tiles);
-    const int kv = part_of / tiles, tile = part_of % tiles;
-    const int group = a.heads / c.heads, queries = min(16, group - 16 * tile);
-    const int head0 = kv * group + 16 * tile;
+    const int parts = c.heads * tiles, group = a.heads / c.heads;
 
-    const KeyRange range = key_range(a, b);
-    const int start = (range.first & ~(kKeys - 1)) + (int)split * a.split_keys;
-    const int end = min(range.n, start + a.split_keys);
-    if (start >= end && a.splits > 1)
-        return;
-
-    const int page0 = start >> c.page_shift;
-    const int count = start < end ? ((end - 1) >> c.page_shift) - page0 + 1 : 0;
-    for (int i = threadIdx.x; i < count; i += 64 * kWaves) {
-        const int32_t id = c.table[b * c.table_stride + page0 + i];
-        ids[i] = id >= 0 && id < c.pages ? id : -1;
-    }
-
-    // Q^T: lane (m, g) holds query m; step s holds the channels that the key
-    // loads below put there
-    v4u qf[kSteps];
+    // ---- this block's run of units
+    Head at;
+    Share share{0, 0};
+    int64_t total = 0;
+    if constexpr (!SHARED) {
+        at.b = blockIdx.x / (uint32_t)parts;
+        at.part = (int)(blockIdx.x % (uint32_t)parts);
+        at.unit = 0;
+    } else {
+        // sequences without keys are in no run
+        for (int64_t b = blockIdx.x; b < c.sequences; b += gridDim.x)
+            if (key_range(a, b, kUnit).units == 0)
+                for (int i = 4 * threadIdx.x; i < a.heads * D; i += 4 * kThreads)
+                    *reinterpret_cast<uint2*>(a.o + b * a.o_token + i / D * a.o_head + i % D) = uint2{0, 0};
+        // prefix sums of the sequences' units, kThreads sequences at a time: the
+        // total first, then where the run begins
+        uint32_t mine = 0, before = 0, sum = 0;      // 2^23 units a sequence at most
+        auto scan = [&](int64_t b0) {
+            const int64_t b = b0 + threadIdx.x;
+            mine = b < c.sequences ? (uint32_t)key_range(a, b, kUnit).units : 0u;
+            uint32_t up = mine;
 #pragma unroll
-    for (int s = 0; s < kSteps; ++s) {
-        const int channel = FP8 ? 64 * (s / 2) + 16 * g + 8 * (s & 1) : 32 * s + 8 * g;
-        qf[s] = m < queries ? *reinterpret_cast<const v4u*>(a.q + b * a.q_token + (head0 + m) * a.q_head + channel)
-                            : v4u{0, 0, 0, 0};
+            for (int d = 1; d < 64; d <<= 1) {
+                const uint32_t other = __shfl_up(up, d);
+                up += lane >= d ? other : 0u;
+            }
+            __syncthreads();
+            if (lane == 63)
+                sums[wave] = up;
+            __syncthreads();
+            before = up - mine;
+            sum = 0;
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) {
+                before += w < wave ? sums[w] : 0u;
+                sum += sums[w];
+            }
+        };
+        for (int64_t b0 = 0; b0 < c.sequences; b0 += kThreads) {
+            scan(b0);
+            total += sum;
+        }
+        total *= parts;
+        share = share_of(total, gridDim.x, blockIdx.x);
+        if (share.count == 0) {
+            if (threadIdx.x == 0)
+                parts_of(a, D)[blockIdx.x] = Part{0, 0, 0, 0, 0};
+            return;
+        }
+        int64_t behind = 0;
+        for (int64_t b0 = 0;; b0 += kThreads) {
+            if (c.sequences > kThreads)
+                scan(b0);
+            const int64_t begin = (behind + before) * parts;
+            if (share.first >= begin && share.first < begin + (int64_t)mine * parts) {
+                found[0] = b0 + threadIdx.x;
+                found[1] = begin;
+            }
+            behind += sum;
+            if (share.first < behind * parts)
+                break;
+        }
+        __syncthreads();
+        at.b = found[0];
+        at.range = key_range(a, at.b, kUnit);
+        const int64_t inside = share.first - found[1];
+        at.part = (int)(inside / at.range.units);
+        at.unit = (int)(inside - (int64_t)at.part * at.range.units);
+        at.count = (int)min(share.count, (int64_t)(at.range.units - at.unit));
     }
-    __syncthreads();
 
+    // the head in work: its pointers, Q^T, sums, and the first step's keys and values
     const float scale = a.scale * 1.4426950408889634f * c.k_scale;
-    v4f acc[kTiles] = {}, sum = {};
-    float top = kNoScore;
-    constexpr int kBytes = FP8 ? 1 : 2;
-    const int64_t head_at = ((int64_t)kv << c.page_shift) * D;
-    const uint8_t* keys = static_cast<const uint8_t*>(c.k) + head_at * kBytes;
-    const uint8_t* values = static_cast<const uint8_t*>(c.v) + head_at * kBytes;
-    const int mask = (1 << c.page_shift) - 1;
+    const int mask = (1 << c.page_shift) - 1, last_page = c.table_pages - 1;
+    const uint8_t *keys, *values;
+    const int32_t* table;
+    int key0, end;
+    v4u qf[kSteps];
+    v4f acc[kTiles], sum;
+    float top;
 
-    for (int key0 = start + kKeys * wave; key0 < end; key0 += kKeys * kWaves) {
-        const int kb = key0 + 8 * (m >> 2), vb = key0 + 8 * g;
-        const int32_t kid = ids[(min(kb, end - 1) >> c.page_shift) - page0];
-        const int32_t vid = vb < end ? ids[(vb >> c.page_shift) - page0] : -1;
-        const uint8_t* kp = keys + ((int64_t)max(kid, 0) * c.page_stride + (int64_t)((kb & mask) + (m & 3)) * D) * kBytes;
-        const uint8_t* vp = values + ((int64_t)max(vid, 0) * c.page_stride + (int64_t)(vb & mask) * D) * kBytes;
-        v4u kf[2][kSteps];
-        uint32_t vr[8][D / 32];
+    // the pages of a step's keys: of key rows m and m + 16, and of value rows 8
+    // g .. of each tile.  Past the sequence's end the table may hold anything.
+    struct Pages {
+        int32_t k[kR], v[kR];
+    };
+    auto find = [&](int key0) {
+        Pages p;
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            if constexpr (FP8) {
+        for (int r = 0; r < kR; ++r) {
+            const int kb = key0 + kKeys * r + 8 * (m >> 2), vb = key0 + kKeys * r + 8 * g;
+            p.k[r] = table[min(kb >> c.page_shift, last_page)];
+            p.v[r] = table[min(vb >> c.page_shift, last_page)];
+        }
+        return p;
+    };
+    auto is_page = [&](int32_t id) { return id >= 0 && id < c.pages; };
+    v4u kr[kR][2][FP8 ? kSteps / 2 : kSteps];
+    uint32_t vr[kR][8][D * kBytes / 64];
+    auto fetch_keys = [&](int key0, const Pages& pages) {
 #pragma unroll
-                for (int s = 0; s < kSteps / 2; ++s) {
-                    const v4u w = *reinterpret_cast<const v4u*>(kp + 4 * t * D + 64 * s + 16 * g);
-                    kf[t][2 * s] = v4u{e4m3_pair(w[0], false), e4m3_pair(w[0], true), e4m3_pair(w[1], false), e4m3_pair(w[1], true)};
-                    kf[t][2 * s + 1] = v4u{e4m3_pair(w[2], false), e4m3_pair(w[2], true), e4m3_pair(w[3], false), e4m3_pair(w[3], true)};
+        for (int r = 0; r < kR; ++r) {
+            const int kb = key0 + kKeys * r + 8 * (m >> 2);
+            const int64_t page = is_page(pages.k[r]) ? pages.k[r] : 0;
+            const uint8_t* p = keys + 16 * g + (page * c.page_stride + (int64_t)((kb & mask) + (m & 3)) * D) * kBytes;
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int s = 0; s < (FP8 ? kSteps / 2 : kSteps); ++s)
+                    kr[r][t][s] = load<D == 128>(p + 4 * t * D * kBytes + 64 * s);
+        }
+    };
+    auto fetch_values = [&](int key0, const Pages& pages) {
+        constexpr int kWords = kRun * kBytes / 4;
+#pragma unroll
+        for (int r = 0; r < kR; ++r) {
+            const int vb = key0 + kKeys * r + 8 * g;
+            const int64_t page = is_page(pages.v[r]) ? pages.v[r] : 0;
+            const uint8_t* p = values + (page * c.page_stride + (int64_t)(vb & mask) * D + kRun * m) * kBytes;
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+#pragma unroll
+                for (int i = 0; i < kTiles / kRun; ++i) {
+                    const auto w = once<kWords>(p + (j * D + 16 * kRun * i) * kBytes);
+#pragma unroll
+                    for (int n = 0; n < kWords; ++n)
+                        vr[r][j][kWords * i + n] = w[n];
                 }
-            } else {
+        }
+    };
+    // S^T of a step, times the scale in units of log2
+    auto score = [&](float (&p)[kR][8]) {
 #pragma unroll
-                for (int s = 0; s < kSteps; ++s)
-                    kf[t][s] = *reinterpret_cast<const v4u*>(kp + (4 * t * D + 32 * s + 8 * g) * 2);
+        for (int r = 0; r < kR; ++r) {
+            v4f s0 = {}, s1 = {};
+#pragma unroll
+            for (int s = 0; s < kSteps; ++s) {
+                v4u k0, k1;
+                if constexpr (FP8) {
+                    const v4u w0 = kr[r][0][s / 2], w1 = kr[r][1][s / 2];
+                    const int n = 2 * (s & 1);
+                    k0 = v4u{e4m3_pair(w0[n], false), e4m3_pair(w0[n], true), e4m3_pair(w0[n + 1], false), e4m3_pair(w0[n + 1], true)};
+                    k1 = v4u{e4m3_pair(w1[n], false), e4m3_pair(w1[n], true), e4m3_pair(w1[n + 1], false), e4m3_pair(w1[n + 1], true)};
+                } else {
+                    k0 = kr[r][0][s];
+                    k1 = kr[r][1][s];
+                }
+                s0 = mfma(k0, qf[s], s0);
+                s1 = mfma(k1, qf[s], s1);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                p[r][i] = s0[i] * scale;
+                p[r][4 + i] = s1[i] * scale;
             }
         }
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const uint8_t* p = vp + (j * D + kTiles * m) * kBytes;
-            if constexpr (FP8) {
-                uint32_t w[D / 64];
-                __builtin_memcpy(w, __builtin_assume_aligned(p, D / 16), D / 16);
-#pragma unroll
-                for (int i = 0; i < D / 64; ++i) {
-                    vr[j][2 * i] = e4m3_pair(w[i], false);
-                    vr[j][2 * i + 1] = e4m3_pair(w[i], true);
-                }
-            } else {
-                __builtin_memcpy(vr[j], __builtin_assume_aligned(p, D == 64 ? 8 : 16), D / 8);
-            }
-        }
-
-        v4f s0 = {}, s1 = {};
-#pragma unroll
-        for (int s = 0; s < kSteps; ++s) {
-            s0 = mfma(kf[0][s], qf[s], s0);
-            s1 = mfma(kf[1][s], qf[s], s1);
-        }
-        float p[8];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            p[i] = s0[i] * scale;
-            p[4 + i] = s1[i] * scale;
-        }
+    };
+    auto accumulate = [&](int key0, float (&p)[kR][8], const Pages& pages) {
         // keys outside the range and pages out of range: no weight, whatever
         // their places hold (a NaN there must not reach either product)
-        if (key0 < range.first || key0 + kKeys > end || !__all(vid >= 0)) {
+        bool all = key0 >= at.range.first && key0 + kStep <= end;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const bool counts = vid >= 0 && vb + j >= range.first && vb + j < end;
-                p[j] = counts ? p[j] : -__builtin_inff();
+        for (int r = 0; r < kR; ++r)
+            all = all && __all(is_page(pages.v[r]));
+        if (!all) {
 #pragma unroll
-                for (int i = 0; i < D / 32; ++i)
-                    vr[j][i] = counts ? vr[j][i] : 0u;
-            }
+            for (int r = 0; r < kR; ++r)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const int key = key0 + kKeys * r + 8 * g + j;
+                    const bool counts = is_page(pages.v[r]) && key >= at.range.first && key < end;
+                    p[r][j] = counts ? p[r][j] : -__builtin_inff();
+#pragma unroll
+                    for (int i = 0; i < D * kBytes / 64; ++i)
+                        vr[r][j][i] = counts ? vr[r][j][i] : 0u;
+                }
         }
-        float most = fmaxf(fmaxf(fmaxf(p[0], p[1]), fmaxf(p[2], p[3])), fmaxf(fmaxf(p[4], p[5]), fmaxf(p[6], p[7])));
+        float most = p[0][0];
+#pragma unroll
+        for (int r = 0; r < kR; ++r)
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                most = fmaxf(most, p[r][j]);
         most = column_max(most);
         if (__any(most > top)) {
             const float next = fmaxf(most, top);
@@ -206,113 +375,223 @@ __global__ __launch_bounds__(64 * kWaves) void paged_attention_kernel(const Page
             sum *= by;
         }
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            p[j] = __builtin_amdgcn_exp2f(p[j] - top);
-        const v4u pf = {pack_bf16(p[0], p[1]), pack_bf16(p[2], p[3]), pack_bf16(p[4], p[5]), pack_bf16(p[6], p[7])};
-        const uint32_t one = 0x3F803F80u;
-        sum = mfma(v4u{one, one, one, one}, pf, sum);
+        for (int r = 0; r < kR; ++r) {
 #pragma unroll
-        for (int t = 0; t < kTiles; ++t) {
-            const uint32_t pick = t & 1 ? 0x07060302u : 0x05040100u;
-            v4u vf;
+            for (int j = 0; j < 8; ++j)
+                p[r][j] = __builtin_amdgcn_exp2f(p[r][j] - top);
+            const v4u pf = {pack_bf16(p[r][0], p[r][1]), pack_bf16(p[r][2], p[r][3]), pack_bf16(p[r][4], p[r][5]),
+                            pack_bf16(p[r][6], p[r][7])};
+            const uint32_t one = 0x3F803F80u;
+            sum = mfma(v4u{one, one, one, one}, pf, sum);
+            // a channel's 8 keys from a word (two channels, e4m3: four) of each key's row
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                vf[j] = __builtin_amdgcn_perm(vr[2 * j + 1][t / 2], vr[2 * j][t / 2], pick);
-            acc[t] = mfma(vf, pf, acc[t]);
+            for (int t = 0; t < kTiles; ++t) {
+                const uint32_t pick = t & 1 ? 0x07060302u : 0x05040100u;
+                v4u vf;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    uint32_t lo, hi;
+                    if constexpr (FP8) {
+                        lo = e4m3_pair(vr[r][2 * j][t / 4], t / 2 & 1);
+                        hi = e4m3_pair(vr[r][2 * j + 1][t / 4], t / 2 & 1);
+                    } else {
+                        lo = vr[r][2 * j][t / 2];
+                        hi = vr[r][2 * j + 1][t / 2];
+                    }
+                    vf[j] = __builtin_amdgcn_perm(hi, lo, pick);
+                }
+                acc[t] = mfma(vf, pf, acc[t]);
+            }
         }
-    }
+    };
 
-    // the four waves' sums
-    if (m < queries) {
+    // Everything of a head up to its first loads.  Q^T: lane (m, g) holds query m;
+    // step s holds the channels that the key loads put there.
+    Pages now, next;
+    auto begin = [&](const Head& x) {
+        const int kv = x.part / tiles, tile = x.part - kv * tiles;
+        const int queries = min(16, group - 16 * tile), head0 = kv * group + 16 * tile;
+        const int64_t head_at = ((int64_t)kv << c.page_shift) * D;
+        keys = static_cast<const uint8_t*>(c.k) + head_at * kBytes;
+        values = static_cast<const uint8_t*>(c.v) + head_at * kBytes;
+        table = c.table + x.b * c.table_stride;
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int t = 0; t < kTiles; ++t)
-                part[wave][m][kTiles * (4 * g + i) + t] = acc[t][i];
-        if (g == 0) {
-            part_m[wave][m] = top;
-            part_l[wave][m] = sum[0];
+        for (int s = 0; s < kSteps; ++s) {
+            const int channel = FP8 ? 64 * (s / 2) + 16 * g + 8 * (s & 1) : 32 * s + 8 * g;
+            qf[s] = m < queries
+                        ? *reinterpret_cast<const v4u*>(a.q + x.b * a.q_token + (head0 + m) * a.q_head + channel)
+                        : v4u{0, 0, 0, 0};
         }
+        now = find(key0);
+        next = find(key0 + kPass);
+        fetch_keys(key0, now);
+        fetch_values(key0, now);
+    };
+
+    if constexpr (SHARED) {
+        key0 = at.range.from + at.unit * kUnit + kStep * wave;
+        begin(at);
+    } else if (a.window == 0) {
+        // no need to know the length for the first step: the table has entries
+        // there, and a page is read whatever it holds
+        key0 = kStep * wave;
+        if (c.table_pages > 0)
+            begin(at);
+        at.range = key_range(a, at.b, kUnit);
+    } else {
+        at.range = key_range(a, at.b, kUnit);
+        key0 = at.range.from + kStep * wave;
+        if (c.table_pages > 0)
+            begin(at);
     }
-    __syncthreads();
-    const int64_t rows = c.sequences * a.heads;
-    for (int at = threadIdx.x * 4; at < queries * D; at += 64 * kWaves * 4) {
-        const int query = at / D, channel = at % D;
-        float high = part_m[0][query];
+    if constexpr (!SHARED)
+        at.count = at.range.units;
+
+    for (int64_t left = share.count;;) {
+        end = min(at.range.n, at.range.from + (at.unit + at.count) * kUnit);
 #pragma unroll
-        for (int w = 1; w < kWaves; ++w)
-            high = fmaxf(high, part_m[w][query]);
-        v4f o = {};
-        float l = 0.0f;
+        for (int t = 0; t < kTiles; ++t)
+            acc[t] = v4f{};
+        sum = v4f{};
+        top = kNoScore;
+        // the next step's keys are asked for as soon as this one's scores have
+        // used the registers, its values when the product has
+        if (key0 < end) {
+            float p[kR][8];
+            for (; key0 + kPass < end; key0 += kPass) {
+                score(p);
+                const Pages after = find(key0 + 2 * kPass);
+                fetch_keys(key0 + kPass, next);
+                accumulate(key0, p, now);
+                fetch_values(key0 + kPass, next);
+                now = next;
+                next = after;
+            }
+            score(p);
+            accumulate(key0, p, now);
+        }
+
+        // the next head of this block's run: its first loads are on their way
+        // while the waves' sums of this one meet
+        const Head done = at;
+        const bool first_head = left == share.count;
+        left -= at.count;
+        if (SHARED && left > 0) {
+            if (++at.part == parts) {
+                at.part = 0;
+                do
+                    at.range = key_range(a, ++at.b, kUnit);
+                while (at.range.units == 0);
+            }
+            at.unit = 0;
+            at.count = (int)min(left, (int64_t)at.range.units);
+            key0 = at.range.from + kStep * wave;
+            begin(at);
+        }
+
+        const int kv = done.part / tiles, tile = done.part - kv * tiles;
+        const int queries = min(16, group - 16 * tile), head0 = kv * group + 16 * tile;
+        if (m < queries) {
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
-            const float by = __builtin_amdgcn_exp2f(part_m[w][query] - high);
-            o += *reinterpret_cast<const v4f*>(&part[w][query][channel]) * by;
-            l += part_l[w][query] * by;
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int t = 0; t < kTiles; ++t)
+                    part_o[wave][m][16 * kRun * (t / kRun) + kRun * (4 * g + i) + t % kRun] = acc[t][i];
+            if (g == 0) {
+                part_m[wave][m] = top;
+                part_l[wave][m] = sum[0];
+            }
         }
-        const int64_t head = head0 + query;
-        if (a.splits == 1) {
-            const float by = l == 0.0f ? 0.0f : c.v_scale / l;
-            *reinterpret_cast<uint2*>(a.o + b * a.o_token + head * a.o_head + channel) =
-                uint2{pack_bf16(o[0] * by, o[1] * by), pack_bf16(o[2] * by, o[3] * by)};
-        } else {
-            const int64_t row = (b * a.heads + head) * a.splits + split;
-            *reinterpret_cast<v4f*>(a.workspace + row * D + channel) = o;
-            if (channel == 0)
-                *reinterpret_cast<f2*>(a.workspace + rows * a.splits * D + row * 2) = f2{high, l};
+        meet();
+        const bool whole = !SHARED || done.count == done.range.units;
+        const int64_t row0 = (2 * (int64_t)blockIdx.x + (first_head ? 0 : 1)) * 16;
+        for (int i = threadIdx.x * 4; i < queries * D; i += kThreads * 4) {
+            const int query = i / D, channel = i % D;
+            float high = part_m[0][query];
+#pragma unroll
+            for (int w = 1; w < kWaves; ++w)
+                high = fmaxf(high, part_m[w][query]);
+            v4f o = {};
+            float l = 0.0f;
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) {
+                const float by = __builtin_amdgcn_exp2f(part_m[w][query] - high);
+                o += *reinterpret_cast<const v4f*>(&part_o[w][query][channel]) * by;
+                l += part_l[w][query] * by;
+            }
+            if (whole) {
+                const float by = l == 0.0f ? 0.0f : c.v_scale / l;
+                *reinterpret_cast<uint2*>(a.o + done.b * a.o_token + (head0 + query) * a.o_head + channel) =
+                    uint2{pack_bf16(o[0] * by, o[1] * by), pack_bf16(o[2] * by, o[3] * by)};
+            } else {
+                *reinterpret_cast<v4f*>(parts_o(a) + (row0 + query) * D + channel) = o;
+                if (channel == 0)
+                    parts_ml(a, D)[row0 + query] = f2{high, l};
+            }
         }
+        if (SHARED && left <= 0 && threadIdx.x == 0) {
+            // this block is the first of those that share its last head: what the join has to know
+            const int rest = done.range.units - done.unit - done.count;
+            Part r{done.b, head0, queries, first_head ? 0 : 1, 0};
+            if (rest > 0 && done.unit == 0)
+                r.blocks = (int)(block_of(total, gridDim.x, share.first + share.count + rest - 1) - blockIdx.x + 1);
+            parts_of(a, D)[blockIdx.x] = r;
+        }
+        if (!SHARED || left <= 0)
+            return;
+        meet();                                  // the sums have been read
     }
 }
 
-// A block joins the runs of one (sequence, head): each thread four channels of
-// every 256 / (D / 4)-th run.
+// Joins the parts of the heads that several blocks worked on: block (i, query)
+// those of a query of the head that began in block i and did not end there.  A
+// thread takes four channels of every kTeams-th part.
 template <int D>
 __global__ __launch_bounds__(256) void paged_join_kernel(const PagedAttention a)
 {
     constexpr int kLanes = D / 4, kTeams = 256 / kLanes;
-    __shared__ float high_of[4];
     __shared__ v4f part[kTeams][kLanes];
-    __shared__ float part_l[kTeams];
-    const int64_t b = blockIdx.x / (uint32_t)a.heads, head = blockIdx.x % (uint32_t)a.heads;
-    const KeyRange range = key_range(a, b);
-    const int from = range.first & ~(kKeys - 1);
-    const int runs = (max(range.n - from, 0) + a.split_keys - 1) / a.split_keys;
-    const int64_t row0 = (b * a.heads + head) * a.splits;
-    const float* o = a.workspace + row0 * D;
-    const f2* ml = reinterpret_cast<const f2*>(a.workspace + a.cache.sequences * a.heads * a.splits * D) + row0;
-
-    float high = kNoScore;
-    for (int i = threadIdx.x; i < runs; i += 256)
-        high = fmaxf(high, ml[i][0]);
-#pragma unroll
-    for (int d = 32; d; d >>= 1)
-        high = fmaxf(high, __shfl_xor(high, d));
-    if ((threadIdx.x & 63) == 0)
-        high_of[threadIdx.x >> 6] = high;
-    __syncthreads();
-    high = fmaxf(fmaxf(high_of[0], high_of[1]), fmaxf(high_of[2], high_of[3]));
-
+    __shared__ float part_m[kTeams], part_l[kTeams];
+    const Part r = parts_of(a, D)[blockIdx.x];
+    const int query = blockIdx.y;
+    if (r.blocks == 0 || query >= r.queries)
+        return;
     const int at = threadIdx.x % kLanes, team = threadIdx.x / kLanes;
     v4f s = {};
-    float l = 0.0f;
-    for (int i = team; i < runs; i += kTeams) {
-        const f2 w = ml[i];
-        const float by = __builtin_amdgcn_exp2f(w[0] - high);
-        s += *reinterpret_cast<const v4f*>(o + (int64_t)i * D + 4 * at) * by;
-        l += w[1] * by;
+    float high = kNoScore, l = 0.0f;
+#pragma unroll 4
+    for (int i = team; i < r.blocks; i += kTeams) {
+        const int64_t row = (2 * ((int64_t)blockIdx.x + i) + (i == 0 ? r.slot : 0)) * 16 + query;
+        const f2 w = parts_ml(a, D)[row];
+        const v4f o = *reinterpret_cast<const v4f*>(parts_o(a) + row * D + 4 * at);
+        const float next = fmaxf(high, w[0]);
+        const float keep = __builtin_amdgcn_exp2f(high - next), by = __builtin_amdgcn_exp2f(w[0] - next);
+        s = s * keep + o * by;
+        l = l * keep + w[1] * by;
+        high = next;
     }
     part[team][at] = s;
-    if (at == 0)
+    if (at == 0) {
+        part_m[team] = high;
         part_l[team] = l;
+    }
     __syncthreads();
     if (team != 0)
         return;
-    for (int i = 1; i < kTeams; ++i) {
-        s += part[i][at];
-        l += part_l[i];
+    float most = high;
+#pragma unroll
+    for (int i = 1; i < kTeams; ++i)
+        most = fmaxf(most, part_m[i]);
+    s = v4f{};
+    l = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kTeams; ++i) {
+        const float by = __builtin_amdgcn_exp2f(part_m[i] - most);
+        s += part[i][at] * by;
+        l += part_l[i] * by;
     }
     const float by = l == 0.0f ? 0.0f : a.cache.v_scale / l;
-    *reinterpret_cast<uint2*>(a.o + b * a.o_token + head * a.o_head + 4 * at) =
+    *reinterpret_cast<uint2*>(a.o + r.b * a.o_token + (r.head0 + query) * a.o_head + 4 * at) =
         uint2{pack_bf16(s[0] * by, s[1] * by), pack_bf16(s[2] * by, s[3] * by)};
 }
 
@@ -322,32 +601,46 @@ template <int D>
 hipError_t launch(const PagedAttention& a, hipStream_t stream)
 {
     const int tiles = tiles_of(a.heads, a.cache.heads);
-    const uint32_t grid = (uint32_t)(a.cache.sequences * a.cache.heads * tiles * a.splits);
+    if (a.shared == 0) {
+        const uint32_t grid = (uint32_t)(a.cache.sequences * a.cache.heads * tiles);
+        if (a.cache.fp8)
+            paged_attention_kernel<D, true, 8, false><<<grid, 512, 0, stream>>>(a, tiles);
+        else
+            paged_attention_kernel<D, false, D == 256 ? 4 : 8, false><<<grid, D == 256 ? 256 : 512, 0, stream>>>(a, tiles);
+        return hipGetLastError();
+    }
     if (a.cache.fp8)
-        paged_attention_kernel<D, true><<<grid, 64 * kWaves, 0, stream>>>(a, tiles);
+        paged_attention_kernel<D, true, 4, true><<<(uint32_t)a.shared, 256, 0, stream>>>(a, tiles);
     else
-        paged_attention_kernel<D, false><<<grid, 64 * kWaves, 0, stream>>>(a, tiles);
-    if (a.splits > 1)
-        paged_join_kernel<D><<<(uint32_t)(a.cache.sequences * a.heads), 256, 0, stream>>>(a);
+        paged_attention_kernel<D, false, 4, true><<<(uint32_t)a.shared, 256, 0, stream>>>(a, tiles);
+    paged_join_kernel<D><<<dim3((uint32_t)a.shared, (uint32_t)std::min(16, a.heads / a.cache.heads)), 256, 0, stream>>>(a);
     return hipGetLastError();
 }
 
 }  // namespace
 
-PagedSplit paged_split(int64_t sequences, int64_t heads, int64_t kv_heads, int64_t d, int64_t longest)
+int paged_blocks(int64_t sequences, int64_t heads, int64_t kv_heads, int64_t d, bool fp8, int64_t longest)
 {
     const int64_t parts = sequences * kv_heads * tiles_of(heads, kv_heads);
-    int64_t keys = (longest * parts + 2047) / 2048;
-    keys = (keys + 127) / 128 * 128;
-    keys = keys < 128 ? 128 : keys > kMostSplitKeys ? kMostSplitKeys : keys;
-    // a window's first key may lie inside a step
-    const int64_t splits = (longest + kKeys - 1 + keys - 1) / keys;
-    return {(int32_t)keys, (int32_t)(splits < 1 ? 1 : splits)};
+    // Few heads: a block a compute unit, whose long runs one after the other the
+    // memory serves best (8 heads of 262143 keys: 162 us, with three 173).  Many:
+    // as many as fit, so that one's change of heads is another's work (512 heads
+    // of 129 to 4096 e4m3 keys: 70 us with one, 59 with two).
+    const int64_t compute_units = device_compute_units();
+    const int64_t resident = compute_units * (4 * parts <= compute_units ? 1 : fits((int)d, fp8));
+    // a window's first key may lie inside a tile
+    const int64_t units = (longest + kKeys - 1 + unit_keys((int)d, fp8) - 1) / unit_keys((int)d, fp8);
+    // A block a head: one launch, and up to two passes (four) of its eight waves.
+    // 32 heads of up to 333 keys: 7.6 us against 9.0 shared; 4 x 8 heads of 1000
+    // keys: 16.9 against 9.9, but 64 x 8 of up to 1000 (e4m3) 23.6 against 25.8.
+    if (longest <= 512 || (longest <= 1024 && parts >= compute_units))
+        return 0;
+    return (int)std::min(resident, parts * units);
 }
 
-size_t paged_attention_bytes(int64_t sequences, int64_t heads, int64_t d, const PagedSplit& s)
+size_t paged_attention_bytes(int64_t d, int blocks)
 {
-    return s.splits > 1 ? (size_t)(sequences * heads * s.splits) * (size_t)(d + 2) * 4 : 0;
+    return (size_t)blocks * (32 * (size_t)(d + 2) * 4 + sizeof(Part));
 }
 
 hipError_t launch_paged_attention(const PagedAttention& a, hipStream_t stream)

@@ -347,16 +347,13 @@ struct PagedAttention {
     const int32_t* lengths;
     float scale;
     int32_t window;           // 0: all keys
-    int32_t split_keys;       // from paged_split
-    int32_t splits;
-    float* workspace;         // paged_attention_workspace_bytes
+    int32_t shared;           // paged_blocks
+    float* workspace;         // paged_attention_bytes
 };
-// keys a block takes and the number of blocks along the longest sequence
-struct PagedSplit {
-    int32_t keys, splits;
-};
-PagedSplit paged_split(int64_t sequences, int64_t heads, int64_t kv_heads, int64_t d, int64_t longest);
-size_t paged_attention_bytes(int64_t sequences, int64_t heads, int64_t d, const PagedSplit& s);
+// Blocks that share the work of a call in equal runs and leave what has to be
+// joined in the workspace (on the current device); 0: a block takes a head.
+int paged_blocks(int64_t sequences, int64_t heads, int64_t kv_heads, int64_t d, bool fp8, int64_t longest);
+size_t paged_attention_bytes(int64_t d, int blocks);
 hipError_t launch_paged_attention(const PagedAttention& a, hipStream_t stream);
 
 // ------------------------------------------------------------ device helpers

@@ -89,6 +89,32 @@ def test_attention(lengths, kv, group, d, page, fp8):
     _check(R.host(o), x, R.host(k), R.host(v), table, lengths, page, **kw)
 
 
+@pytest.mark.parametrize("S,group,fp8,d", [(300, 2, False, 64), (600, 1, True, 128), (257, 17, False, 64)])
+def test_many_sequences(S, group, fp8, d):
+    """More sequences than a block counts at a time, runs of empty ones, and one long one among them."""
+    import paper_2509_26436_amd as q
+    print(f"paged attention of {S} sequences, group {group} fp8 {fp8} d {d}", flush=True)
+    rng = _rng(11, S)
+    lengths = rng.integers(0, 70, S)
+    lengths[:3], lengths[250:259], lengths[-2:] = 0, 0, 0
+    lengths[S // 2], lengths[255], lengths[256] = 1500, 129, 600
+    lengths = lengths.tolist()
+    _, table, k, v, x, cache = _attention_case(12, lengths, 1, group, d, 32, fp8)
+    o = q.paged_attention(R.device(x), cache, _int32(lengths))
+    _check(R.host(o), x, R.host(k), R.host(v), table, lengths, 32)
+
+
+@pytest.mark.parametrize("kv,group,d,fp8", [(300, 1, 64, False), (64, 3, 128, True)])
+def test_many_short_heads(kv, group, d, fp8):
+    """Heads enough for a block each, over more keys than one pass of it."""
+    import paper_2509_26436_amd as q
+    lengths = [1000, 0, 513, 31, 770]
+    _, table, k, v, x, cache = _attention_case(13, lengths, kv, group, d, 16, fp8)
+    o = q.paged_attention(R.device(x), cache, _int32(lengths))
+    assert q.paged_attention_workspace(5, kv * group, cache) is None
+    _check(R.host(o), x, R.host(k), R.host(v), table, lengths, 16)
+
+
 @pytest.mark.parametrize("window", [1, 7, 32, 100, 5000])
 @pytest.mark.parametrize("fp8", [False, True])
 def test_window_and_scale(window, fp8):
@@ -121,6 +147,106 @@ def test_places_that_do_not_count_hold_nan(fp8, d):
         v[bad & (torch.rand(v.shape, device="cuda") < 0.5)] = math.inf
     o = q.paged_attention(R.device(x), cache, _int32(lengths), window=window)
     _check(R.host(o), x, kh, vh, table, lengths, page, window=window)
+
+
+@pytest.mark.parametrize("kv,group,d,fp8", [(2, 3, 128, False), (1, 20, 64, True), (1, 2, 256, False)])
+@pytest.mark.parametrize("window", [0, 1500])
+def test_long_sequences_with_holes(kv, group, d, fp8, window):
+    """Sequences shared by blocks: NaN wherever nothing counts, pages that are none, lengths below 0
+    and past the table, a window that begins inside a page."""
+    import torch
+    import paper_2509_26436_amd as q
+    page, width = 16, 160
+    lengths = [2300, 0, 1, 1700, 2560, 95, 2560]
+    rng, table, k, v, x, cache = _attention_case(14, lengths, kv, group, d, page, fp8, width=width)
+    table[0, 20:60] = -1
+    table[3, :] = 2 ** 31 - 1
+    table[4, 100] = k.shape[0]
+    table[4, 0:99] = -5
+    cache = q.PagedCache(k, v, _int32(table))
+    kh, vh = R.host(k), R.host(v)
+    have = []
+    counts = np.zeros((k.shape[0], page), bool)
+    for b, n in enumerate(lengths):
+        places = [(table[b, p // page], p % page) for p in range(max(0, n - window) if window else 0, n)
+                  if 0 <= table[b, p // page] < k.shape[0]]
+        have.append(places)
+        for place in places:
+            counts[place] = True
+    bad = torch.from_numpy(~counts).cuda()[:, None, :, None].expand(k.shape)
+    raw = torch.full((), math.nan, dtype=torch.bfloat16, device="cuda").to(k.dtype)
+    bits = torch.uint8 if fp8 else torch.int16
+    for t in (k, v):
+        t.view(bits)[bad] = raw.view(bits)
+    asked = list(lengths)
+    asked[1], asked[6] = -9, 2 ** 31 - 1
+    o = R.host(q.paged_attention(R.device(x), cache, _int32(asked), window=window))
+    for b, places in enumerate(have):
+        at = tuple(np.array(places, np.int64).reshape(-1, 2).T)
+        for h in range(kv):
+            rows = slice(h * group, (h + 1) * group)
+            want, far = R.attention(x[b, rows], kh[:, h][at], vh[:, h][at], 1 / math.sqrt(d))
+            assert (np.abs(o[b, rows] - want) <= far).all(), (b, h)
+    assert (o[1] == 0).all() and (o[3] == 0).all()
+
+
+def test_infinities_in_long_sequences():
+    """The parts of a shared sequence join as one softmax: a whole part of score -inf has no weight,
+    +inf gives NaN, a NaN query gives NaN in its own head only, NaN in a counted value its column."""
+    import torch
+    import paper_2509_26436_amd as q
+    lengths, page = [3000, 3000, 3000], 16
+    _, table, k, v, x, cache = _attention_case(15, lengths, 1, 2, 64, page, False)
+    x = np.abs(x)
+    x[0, 1, 5] = np.nan
+    v[int(table[0, 100]), 0, 3, 9] = math.nan
+    k[int(table[1, 130]), 0, 3, 8] = math.inf
+    lost = torch.from_numpy(table[2, :100]).cuda()
+    k[lost, 0, :, 8] = -math.inf
+    o = R.host(q.paged_attention(R.device(x), cache, _int32(lengths)))
+    assert np.isnan(o[0, 1]).all() and np.isnan(o[0, 0, 9]) and np.isnan(o[0, 0]).sum() == 1
+    assert np.isnan(o[1]).all()
+    kh, vh = (_gather(R.host(t), table, 2, 0, 3000, page)[100 * page:] for t in (k, v))
+    want, far = R.attention(x[2], kh, vh, 1 / math.sqrt(64))
+    assert (np.abs(o[2] - want) <= far).all()
+
+
+def test_tables_without_pages():
+    """A table of no columns, no sequences at all; a cache of no pages is refused."""
+    import torch
+    import paper_2509_26436_amd as q
+    k = torch.full((1, 2, 16, 64), math.nan, dtype=torch.bfloat16, device="cuda")
+    x = torch.ones((3, 4, 64), dtype=torch.bfloat16, device="cuda")
+    lengths = _int32([5, 0, 3000])
+    for table in (np.zeros((3, 0)), np.full((3, 200), -1)):
+        assert (q.paged_attention(x, q.PagedCache(k, k.clone(), _int32(table)), lengths) == 0).all()
+    cache = q.PagedCache(k, k.clone(), _int32(np.zeros((0, 8))))
+    assert q.paged_attention(x[:0], cache, lengths[:0]).shape == (0, 4, 64)
+    with pytest.raises(q.QuartzError):
+        q.paged_attention(x, q.PagedCache(k[:0], k[:0], _int32(np.full((3, 200), -1))), lengths)
+
+
+def test_two_streams_at_once():
+    """Calls on two streams with workspaces of their own, while both run."""
+    import torch
+    import paper_2509_26436_amd as q
+    lengths, page = [5000, 100, 2222], 16
+    _, table, k, v, x, cache = _attention_case(16, lengths, 2, 4, 128, page, False)
+    xs = [R.device(x), R.device(-x)]
+    at = _int32(lengths)
+    want = [q.paged_attention(t, cache, at) for t in xs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in xs]
+    outs = [[], []]
+    for _ in range(20):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                outs[i].append(q.paged_attention(xs[i], cache, at))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for o in outs[i]:
+            assert torch.equal(o, want[i])
+    _check(R.host(want[0]), x, R.host(k), R.host(v), table, lengths, page)
 
 
 def test_lengths_and_pages_out_of_range():
