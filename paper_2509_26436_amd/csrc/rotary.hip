@@ -13,9 +13,10 @@
 // + 8 for the interleaved one; the other channels are copied 16 at a time).
 // A thread keeps its unit's eight sines and cosines over several heads.  Both
 // kernels are bound by memory traffic: two vectors in, two out a unit, and the
-// sines and cosines of a thread are shared by four heads.  V = 1 is the same
-// with single channels in place of vectors, for strides, alignments and
-// numbers of channels that are no multiples of 8 (16).
+// sines and cosines of a thread are shared by four heads.  V = 2 and V = 1 are
+// the same with pairs of channels and single ones in place of vectors, for
+// strides, alignments and numbers of channels that are no multiples of 8 (16),
+// or of 2 (4).
 #include "quartz_internal.h"
 
 namespace quartz {
@@ -38,6 +39,10 @@ __device__ __forceinline__ void load(const uint16_t* p, float (&v)[V])
             v[2 * i] = __uint_as_float(d[i] << 16);
             v[2 * i + 1] = __uint_as_float(d[i] & 0xFFFF0000u);
         }
+    } else if constexpr (V == 2) {
+        const uint32_t w = *reinterpret_cast<const uint32_t*>(p);
+        v[0] = __uint_as_float(w << 16);
+        v[1] = __uint_as_float(w & 0xFFFF0000u);
     } else {
         v[0] = __uint_as_float((uint32_t)*p << 16);
     }
@@ -52,30 +57,54 @@ __device__ __forceinline__ void store(uint16_t* p, const float (&v)[V])
         for (int i = 0; i < 4; ++i)
             d[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f2{v[2 * i], v[2 * i + 1]}, bf2));
         *reinterpret_cast<uint4*>(p) = uint4{d[0], d[1], d[2], d[3]};
+    } else if constexpr (V == 2) {
+        *reinterpret_cast<uint32_t*>(p) = __builtin_bit_cast(uint32_t, __builtin_convertvector(f2{v[0], v[1]}, bf2));
     } else {
         *p = __builtin_bit_cast(uint16_t, (__bf16)v[0]);
     }
 }
 
+// x / scale from inverse = 1 / scale: the product, corrected by its remainder,
+// which the second operation forms without an error.  A quotient that fp32 holds
+// comes out as it is, so that a tie of the rounding to the cache's type is one
+// (the compiler's division has twice the instructions, which is what bounds an
+// e4m3 append: 4612 tokens of 8 x 128 12.0 us with it, 8.9 so).  An infinite
+// product has no remainder; where the quotient is clamped at 448 (LOW) the product
+// is at 1024, and x itself brings infinities and NaN back.
+template <bool LOW>
+__device__ __forceinline__ float quotient(float x, float scale, float inverse)
+{
+    float q = x * inverse;
+    if constexpr (LOW)
+        q = __builtin_amdgcn_fmed3f(q, -1024.0f, 1024.0f);
+    // signs so that a zero keeps its own
+    const float better = __builtin_fmaf(__builtin_fmaf(q, scale, -x), -inverse, q);
+    return LOW || better == better ? better : q;
+}
+
 // e4m3, round to nearest even, saturating at 448; NaN stays NaN
 __device__ __forceinline__ float e4m3_range(float v)
 {
-    const float c = fminf(fmaxf(v, -448.0f), 448.0f);
-    return v == v ? c : v;
+    return __builtin_elementwise_minimum(__builtin_elementwise_maximum(v, -448.0f), 448.0f);
+}
+
+__device__ __forceinline__ uint2 e4m3_eight(const float (&v)[8])
+{
+    uint32_t d[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        int w = __builtin_amdgcn_cvt_pk_fp8_f32(e4m3_range(v[4 * i]), e4m3_range(v[4 * i + 1]), 0, false);
+        d[i] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(e4m3_range(v[4 * i + 2]), e4m3_range(v[4 * i + 3]), w, true);
+    }
+    return uint2{d[0], d[1]};
 }
 
 template <int V>
 __device__ __forceinline__ void store(uint8_t* p, const float (&v)[V])
 {
-    if constexpr (V == 8) {
-        uint32_t d[2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            int w = __builtin_amdgcn_cvt_pk_fp8_f32(e4m3_range(v[4 * i]), e4m3_range(v[4 * i + 1]), 0, false);
-            d[i] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(e4m3_range(v[4 * i + 2]),
-                                                            e4m3_range(v[4 * i + 3]), w, true);
-        }
-        *reinterpret_cast<uint2*>(p) = uint2{d[0], d[1]};
+    if constexpr (V == 2) {
+        *reinterpret_cast<uint16_t*>(p) =
+            (uint16_t)__builtin_amdgcn_cvt_pk_fp8_f32(e4m3_range(v[0]), e4m3_range(v[1]), 0, false);
     } else {
         *p = (uint8_t)__builtin_amdgcn_cvt_pk_fp8_f32(e4m3_range(v[0]), 0.0f, 0, false);
     }
@@ -197,20 +226,13 @@ __global__ __launch_bounds__(kThreads) void paged_append_kernel(const PagedAppen
     const int32_t page = c.table[sequence * c.table_stride + (position >> c.page_shift)];
     if (page < 0 || page >= c.pages)
         return;
-    Unit<V> w;
-    if (values) {
-        w.turned = false;
-        w.at0 = 2 * V * (int)u;
-        w.at1 = w.at0 + V;
-    } else {
-        w = make_unit<V>((int)u, a.rot, a.interleaved, position, a.freqs, a.magnitude, false);
-    }
-    const uint16_t* x = (values ? a.v : a.k) + (int64_t)token * (values ? a.v_token : a.k_token);
-    const int64_t x_head = values ? a.v_head : a.k_head;
+    const Unit<V> w = make_unit<V>((int)u, values ? 0 : a.rot, a.interleaved, position, a.freqs, a.magnitude, false);
     T* y = static_cast<T*>(values ? c.v : c.k) + page * c.page_stride +
            (int64_t)(position & ((1 << c.page_shift) - 1)) * c.d;
     const int64_t y_head = (int64_t)c.d << c.page_shift;
-    const float scale = values ? c.v_scale : c.k_scale;
+    const float scale = values ? c.v_scale : c.k_scale, inverse = 1.0f / scale;
+    const uint16_t* x = (values ? a.v : a.k) + (int64_t)token * (values ? a.v_token : a.k_token);
+    const int64_t x_head = values ? a.v_head : a.k_head;
     const int first = (int)group * kHeadsPerThread;
     float v0[kHeadsPerThread][V], v1[kHeadsPerThread][V];
 #pragma unroll
@@ -227,16 +249,36 @@ __global__ __launch_bounds__(kThreads) void paged_append_kernel(const PagedAppen
         if (scale != 1.0f) {
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                v0[i][j] = v0[i][j] / scale;      // the correctly rounded quotient: its ties are the e4m3 rounding's
-                v1[i][j] = v1[i][j] / scale;
+                v0[i][j] = quotient<sizeof(T) == 1>(v0[i][j], scale, inverse);
+                v1[i][j] = quotient<sizeof(T) == 1>(v1[i][j], scale, inverse);
             }
         }
-        store<V>(y + (first + i) * y_head + w.at0, v0[i]);
-        store<V>(y + (first + i) * y_head + w.at1, v1[i]);
+        T* to = y + (first + i) * y_head;
+        if constexpr (V == 8 && sizeof(T) == 1) {
+            const uint2 d0 = e4m3_eight(v0[i]), d1 = e4m3_eight(v1[i]);
+            if (w.at1 == w.at0 + V) {            // a run of 16: one store
+                *reinterpret_cast<uint4*>(to + w.at0) = uint4{d0.x, d0.y, d1.x, d1.y};
+            } else {
+                *reinterpret_cast<uint2*>(to + w.at0) = d0;
+                *reinterpret_cast<uint2*>(to + w.at1) = d1;
+            }
+        } else {
+            store<V>(to + w.at0, v0[i]);
+            store<V>(to + w.at1, v1[i]);
+        }
     }
 }
 
-bool vector16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+// Channels of a vector: the most of 8, 2 and 1 that pairs, heads, strides and
+// pointers allow (4608 tokens of 32 x 128, all turned: 14.2 us with 8; 20 of them
+// turned: 15.4 us with 2, 21.6 with 1).
+int vector_of(int d, int rot, uintptr_t pointers, int64_t strides)
+{
+    for (int v : {8, 2})
+        if (d % (2 * v) == 0 && rot % (2 * v) == 0 && pointers % (2 * v) == 0 && (strides & (v - 1)) == 0)
+            return v;
+    return 1;
+}
 
 uint32_t blocks_of(int64_t threads) { return (uint32_t)((threads + kThreads - 1) / kThreads); }
 
@@ -246,15 +288,17 @@ hipError_t launch_rotary(const Rotary& a, hipStream_t stream)
 {
     const int64_t groups = (a.heads + kHeadsPerThread - 1) / kHeadsPerThread;
     const bool in_place = a.x == a.y;
-    const bool vectors = a.d % 16 == 0 && a.rot % 16 == 0 && vector16(a.x) && vector16(a.y) &&
-                         ((a.x_token | a.x_head | a.y_token | a.y_head) & 7) == 0;
     const int channels = in_place ? a.rot : a.d;
-    const int64_t units = vectors ? channels / 16 : channels / 2;
+    const int64_t strides = a.x_token | a.x_head | a.y_token | a.y_head;
+    const int v = vector_of(a.d, a.rot, reinterpret_cast<uintptr_t>(a.x) | reinterpret_cast<uintptr_t>(a.y), strides);
+    const int64_t units = channels / (2 * v);
     if (units == 0)
         return hipSuccess;
     const uint32_t grid = blocks_of(a.tokens * groups * units);
-    if (vectors)
+    if (v == 8)
         rotary_kernel<8><<<grid, kThreads, 0, stream>>>(a, (uint32_t)units, (uint32_t)groups);
+    else if (v == 2)
+        rotary_kernel<2><<<grid, kThreads, 0, stream>>>(a, (uint32_t)units, (uint32_t)groups);
     else
         rotary_kernel<1><<<grid, kThreads, 0, stream>>>(a, (uint32_t)units, (uint32_t)groups);
     return hipGetLastError();
@@ -264,12 +308,14 @@ template <typename T>
 static hipError_t launch_append(const PagedAppend& a, hipStream_t stream)
 {
     const int64_t groups = (a.cache.heads + kHeadsPerThread - 1) / kHeadsPerThread;
-    const bool vectors = a.rot % 16 == 0 && vector16(a.k) && vector16(a.v) &&
-                         ((a.k_token | a.k_head | a.v_token | a.v_head) & 7) == 0;
-    const int64_t units = vectors ? a.cache.d / 16 : a.cache.d / 2;
+    const int v = vector_of(a.cache.d, a.rot, reinterpret_cast<uintptr_t>(a.k) | reinterpret_cast<uintptr_t>(a.v),
+                            a.k_token | a.k_head | a.v_token | a.v_head);
+    const int64_t units = a.cache.d / (2 * v);
     const uint32_t grid = blocks_of(a.tokens * 2 * groups * units);
-    if (vectors)
+    if (v == 8)
         paged_append_kernel<T, 8><<<grid, kThreads, 0, stream>>>(a, (uint32_t)units, (uint32_t)groups);
+    else if (v == 2)
+        paged_append_kernel<T, 2><<<grid, kThreads, 0, stream>>>(a, (uint32_t)units, (uint32_t)groups);
     else
         paged_append_kernel<T, 1><<<grid, kThreads, 0, stream>>>(a, (uint32_t)units, (uint32_t)groups);
     return hipGetLastError();

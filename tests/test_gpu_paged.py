@@ -457,6 +457,34 @@ def test_append_keeps_nan_and_saturates():
         assert abs(got[7] - 0.001) <= 2.0 ** -10
 
 
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("scale", [0.75, 1.1, 0.0371, 1.5 * 2.0 ** -126, 1.5 * 2.0 ** 126, 3.3e38])
+def test_append_divides_every_value(scale, fp8):
+    """Every bf16 value over a scale: the fp32 quotient, rounded to the cache's type, bit for bit.
+    Below 2^-120 the quotient's remainder is no fp32 number any more, and over a scale past 2^126 the
+    reciprocal is subnormal: there a value may fall to the neighbour."""
+    import torch
+    import paper_2509_26436_amd as q
+    bits = torch.arange(1 << 16, dtype=torch.int32).to(torch.int16)
+    x = bits.view(torch.bfloat16).view(512, 1, 128).cuda()
+    dtype = torch.float8_e4m3fn if fp8 else torch.bfloat16
+    k = torch.zeros((32, 1, 16, 128), dtype=torch.bfloat16, device="cuda").to(dtype)
+    cache = q.PagedCache(k, torch.zeros_like(k.view(torch.uint8)).view(dtype), _int32([range(32)]), scale, scale)
+    q.paged_append(cache, x, x, _int32(range(512)), _int32([0] * 512))
+    with np.errstate(all="ignore"):
+        want = x.cpu().float().numpy() / np.float32(scale)
+    want = torch.from_numpy(np.clip(want, -448, 448) if fp8 else want).to(dtype).view(-1)
+    code = torch.uint8 if fp8 else torch.int16
+    small = (x.cpu().float().abs().view(-1) < 2.0 ** -120) | (scale > 2.0 ** 126)
+    for t in (cache.k, cache.v):
+        got = t.cpu().view(-1)
+        a, b = got.view(code).int(), want.view(code).int()
+        both_nan = got.float().isnan() & want.float().isnan()
+        assert (got.float().isnan() == want.float().isnan()).all()
+        off = torch.where(both_nan, 0, (a - b).abs())
+        assert (off[~small] == 0).all() and off.max() <= 1
+
+
 @pytest.mark.parametrize("T", [0, 1])
 def test_append_without_sequences_or_tokens(T):
     import torch
