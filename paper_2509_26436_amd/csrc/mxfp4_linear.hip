@@ -423,29 +423,48 @@ __global__ __launch_bounds__(256) void mxfp4_tiled_kernel(const MxLinear a, uint
         last_step(One());
     }
 
+    // the bias of this lane's columns, all of it on its way at once
+    v4i bias[TN][2];
+#pragma unroll
+    for (int t = 0; t < TN; ++t)
+        bias[t][0] = bias[t][1] = v4i{0, 0, 0, 0};
+    if (a.bias && a.N - n0 >= kN && (reinterpret_cast<uintptr_t>(a.bias) & 15) == 0) {
+#pragma unroll
+        for (int t = 0; t < TN; ++t)
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                bias[t][i] = *reinterpret_cast<const v4i*>(a.bias + n0 + wn + 32 * t + 16 * h + 8 * i);
+    } else if (a.bias) {
+#pragma unroll
+        for (int t = 0; t < TN; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int64_t n = min(n0 + wn + 32 * t + 16 * h + i, a.N - 1);
+                bias[t][i / 8][i % 8 / 2] |= (int)((uint32_t)a.bias[n] << (16 * (i & 1)));
+            }
+    }
 #pragma unroll
     for (int t = 0; t < TN; ++t) {
         const int64_t n = n0 + wn + 32 * t + 16 * h;
         const int count = (int)max((int64_t)0, min((int64_t)16, a.N - n));
-        float bias[16];
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-            bias[i] = a.bias && i < count ? bf16_value(a.bias[n + i]) : 0.0f;
 #pragma unroll
         for (int u = 0; u < TM; ++u) {
             const int64_t m = m0 + wm - kN + 32 * u + r;
+            float v[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                v[i] = acc[t][u][i] + bf16_value((uint16_t)((uint32_t)bias[t][i / 8][i % 8 / 2] >> (16 * (i & 1))));
+            if (a.gelu) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    v[i] = gelu_tanh(v[i]);
+            }
             if (m >= a.M || count == 0)
                 continue;
             uint32_t out[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                float lo = acc[t][u][2 * i] + bias[2 * i], hi = acc[t][u][2 * i + 1] + bias[2 * i + 1];
-                if (a.gelu) {
-                    lo = gelu_tanh(lo);
-                    hi = gelu_tanh(hi);
-                }
-                out[i] = pack_bf16(lo, hi);
-            }
+            for (int i = 0; i < 8; ++i)
+                out[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
             uint16_t* dst = a.y + m * a.ldy + n;
             if (count == 16 && (a.ldy & 7) == 0) {
                 reinterpret_cast<uint4*>(dst)[0] = uint4{out[0], out[1], out[2], out[3]};
@@ -483,6 +502,9 @@ bool mxfp4_fuses(int64_t M, int64_t K) { return M <= kFusedRows && M * K <= kFus
 // with 256 x 256); 4096 tokens 43 with 128 x 128 and 37 with 256 x 256.  Tiles
 // of 192 serve what they fill whole rounds of: 4608 x 8192 x 8192 takes 151 us
 // with 192 x 256 (three rounds) and 168 with 256 x 256 (two and a quarter).
+// Where K is short, two blocks a compute unit hide each other's stores: 18432 x
+// 4608 at K = 1152 takes 89 us in tiles of 128 x 128 (97 with bias and GELU) and
+// 90 (107) in those of 192 x 256, at K = 4608 239 and 220.
 MxShape mxfp4_shape(int64_t M, int64_t N, int64_t K)
 {
     if (M <= 16)
@@ -502,9 +524,10 @@ MxShape mxfp4_shape(int64_t M, int64_t N, int64_t K)
     };
     consider({false, 4, 4}, 2.5 + 0.15 * kk + medium * (8.6 + 3.15 * kk) / 1000);
     const double each = blocks(128, 128), x = each <= 512 ? each / 256 : 2 * std::ceil(each / 512);
-    consider({true, 2, 2}, 4 + 1.6 * x + kk * std::max(2.1, 2.0 * x));
+    consider({true, 2, 2}, 3.5 + 1.4 * x + kk * std::max(2.1, 2.05 * x));
     for (const MxShape& s : {MxShape{true, 3, 4}, MxShape{true, 4, 3}, MxShape{true, 4, 4}})
-        consider(s, 4 + std::ceil(blocks(64 * s.tm, 64 * s.tn) / 256) * s.tm * s.tn * (0.5 + 0.4 * kk));
+        consider(s, 2 + std::ceil(blocks(64 * s.tm, 64 * s.tn) / 256) *
+                            (0.5 * s.tm * s.tn + kk * (s.tm * s.tn == 16 ? 6.6 : 5.7)));
     return best;
 }
 

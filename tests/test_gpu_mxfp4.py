@@ -126,7 +126,8 @@ def test_linear(M, N, K, act, with_bias):
 @pytest.mark.parametrize("M,N,K,tile", [(2048, 2048, 256, (128, 128)), (1999, 2100, 320, (128, 128)),
                                         (4090, 4093, 64, (128, 128)), (4000, 1100, 2112, (128, 128)),
                                         (4090, 4093, 1216, (256, 256)), (4090, 4093, 2048, (256, 256)),
-                                        (2304, 4100, 1152, (192, 256)), (4600, 8190, 448, (192, 256)),
+                                        (2304, 4100, 1152, (192, 256)), (2300, 4100, 448, (192, 256)),
+                                        (4600, 8190, 448, (128, 128)),
                                         (8190, 4599, 832, (256, 192)),
                                         (200, 4000, 2112, (32, 32)), (300, 3001, 4096, (64, 64))])
 def test_linear_large(M, N, K, tile):
