@@ -178,13 +178,28 @@ __global__ __launch_bounds__(kDirectThreads) void mxfp4_direct_kernel(const MxLi
             load(first + kDirectWaves * kAhead);
     }
 
+    // wave w finishes tiles w, w + 8, ...: their bias is on its way while the sums meet
+    constexpr int kMine = (TN * TM + kDirectWaves - 1) / kDirectWaves;
+    v4f bias[kMine] = {};
+    if (a.bias) {
+#pragma unroll
+        for (int j = 0; j < kMine; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                bias[j][i] = bf16_value(
+                    a.bias[min(n0 + 4 * TN * g + 4 * ((wave + kDirectWaves * j) / TM) + i, a.N - 1)]);
+    }
 #pragma unroll
     for (int t = 0; t < TN; ++t)
 #pragma unroll
         for (int u = 0; u < TM; ++u)
             part[wave][t * TM + u][lane] = acc[t][u];
     __syncthreads();
-    for (int tile = wave; tile < TN * TM; tile += kDirectWaves) {
+#pragma unroll
+    for (int j = 0; j < kMine; ++j) {
+        const int tile = wave + kDirectWaves * j;
+        if (tile >= TN * TM)
+            break;
         v4f s = part[0][tile][lane];
 #pragma unroll
         for (int w = 1; w < kDirectWaves; ++w)
@@ -197,8 +212,7 @@ __global__ __launch_bounds__(kDirectThreads) void mxfp4_direct_kernel(const MxLi
         const int count = (int)min((int64_t)4, a.N - n);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            if (a.bias && i < count)
-                s[i] += bf16_value(a.bias[n + i]);
+            s[i] += bias[j][i];
             if (a.gelu)
                 s[i] = gelu_tanh(s[i]);
         }
