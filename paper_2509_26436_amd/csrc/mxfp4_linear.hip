@@ -442,7 +442,7 @@ __global__ __launch_bounds__(256) void mxfp4_tiled_kernel(const MxLinear a, uint
 #pragma unroll
     for (int t = 0; t < TN; ++t)
         bias[t][0] = bias[t][1] = v4i{0, 0, 0, 0};
-    if (a.bias && a.N - n0 >= kN && (reinterpret_cast<uintptr_t>(a.bias) & 15) == 0) {
+    if (a.bias && a.N - n0 >= kN) {
 #pragma unroll
         for (int t = 0; t < TN; ++t)
 #pragma unroll
@@ -528,15 +528,18 @@ MxShape mxfp4_shape(int64_t M, int64_t N, int64_t K)
         return (double)((M + rows - 1) / rows) * (double)((N + columns - 1) / columns);
     };
     const double small = std::max(blocks(32, 32), 256.0), medium = std::max(blocks(64, 64), 256.0);
-    MxShape best{false, 2, 2};
-    double least = 2.5 + 0.1 * kk + small * (1.4 + 1.25 * kk) / 1000;
+    // (a direct grid has at most 65535 blocks of tokens)
+    const bool direct = M <= 65535 * 32;
+    MxShape best{!direct, 2, 2};
+    double least = direct ? 2.5 + 0.1 * kk + small * (1.4 + 1.25 * kk) / 1000 : INFINITY;
     auto consider = [&](const MxShape& s, double time) {
         if (time < least) {
             best = s;
             least = time;
         }
     };
-    consider({false, 4, 4}, 2.5 + 0.15 * kk + medium * (8.6 + 3.15 * kk) / 1000);
+    if (direct)
+        consider({false, 4, 4}, 2.5 + 0.15 * kk + medium * (8.6 + 3.15 * kk) / 1000);
     const double each = blocks(128, 128), x = each <= 512 ? each / 256 : 2 * std::ceil(each / 512);
     consider({true, 2, 2}, 3.5 + 1.4 * x + kk * std::max(2.1, 2.05 * x));
     for (const MxShape& s : {MxShape{true, 3, 4}, MxShape{true, 4, 3}, MxShape{true, 4, 4}})

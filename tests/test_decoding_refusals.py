@@ -69,6 +69,9 @@ def test_mxfp4_linear_kernel():
             (1024, 4096, 4096, "tiled", 128, 128, False), (4096, 4096, 4096, "tiled", 256, 256, False),
             (4608, 8192, 8192, "tiled", 192, 256, False), (8192, 4608, 8192, "tiled", 256, 192, False)):
         assert q.mxfp4_linear_kernel(M, N, K) == {"kernel": kernel, "rows": rows, "cols": cols, "fused": fused}
+    # more tokens than a direct kernel's grid holds
+    for M in (1 << 22, 1 << 28):
+        assert q.mxfp4_linear_kernel(M, 16, 64)["kernel"] == "tiled"
     assert q.quartz_mxfp4_linear_kernel(0, 8, 64, A) == q.quartz_mxfp4_linear_kernel(8, 8, 96, A) == ESHAPE
     assert q.quartz_mxfp4_linear_kernel(8, 8, 64, None) == ENULL
 

@@ -217,3 +217,37 @@ def test_graph_stream_and_shared_workspace(M):
         torch.cuda.synchronize()
         assert torch.equal(out, want[i])
         assert torch.equal(q.mxfp4_linear(xs[i - 1], w, workspace=ws), want[i - 1])
+
+
+@pytest.mark.parametrize("M,K,kernel", [(65535 * 32, 64, "direct"), (65535 * 32 + 1, 64, "tiled"),
+                                        ((1 << 32) // 512 + 40, 1024, "tiled")])
+def test_very_many_tokens(M, K, kernel):
+    """As many tokens as a direct kernel's grid holds, one more, and codes past 2^32 bytes: rows from
+    all over against the same rows by themselves."""
+    import torch
+    import paper_2509_26436_amd as q
+    print(f"mxfp4 {M} tokens x {K}", flush=True)
+    assert q.mxfp4_linear_kernel(M, 20, K)["kernel"] == kernel
+    rng = _rng(8, M)
+    rows = np.unique(np.r_[0:40, M - 60:M, rng.integers(0, M, 100)])
+    some = R.device(_tokens(rng, len(rows), K, 1.0))
+    at = torch.from_numpy(rows).cuda()
+    x = torch.zeros((M, K), dtype=torch.bfloat16, device="cuda")
+    x[at] = some
+    w = q.mxfp4_quantize(R.device(R.bf16(rng.normal(0, 0.05, (20, K)))))
+    bias = R.device(R.bf16(rng.normal(0, 1, 20)))
+    t, few = q.mxfp4_quantize(x), q.mxfp4_quantize(some)
+    assert torch.equal(t.codes[:, at], few.codes) and torch.equal(t.scales[:, at], few.scales)
+    y, want = q.mxfp4_linear(t, w, bias), q.mxfp4_linear(few, w, bias)
+    # the kernels differ in the order of their sums, which fp32 rounds: at most K 2^-24 of the
+    # products' magnitudes, then one rounding to bf16 on either side
+    far = (q.mxfp4_dequantize(few).double().abs() @ q.mxfp4_dequantize(w).double().abs().T + bias.double().abs()) * K * 2.0 ** -23
+    off = (y[at].double() - want.double()).abs()
+    assert (off <= far + want.double().abs() * 2.0 ** -7 + far * 2.0 ** -7).all()
+    del x
+    back = q.mxfp4_dequantize(t)
+    assert torch.equal(back[at], q.mxfp4_dequantize(few))
+    mask = torch.ones(M, dtype=torch.bool, device="cuda")
+    mask[at] = False
+    assert not back.view(torch.int16).any(1).logical_and(mask).any()
+    assert (y[mask][:1000] == bias).all()
