@@ -378,6 +378,7 @@ quartz_status quartz_paged_attention(const void* q_bf16, void* o_bf16, int64_t s
     a.scale = scale;
     a.window = (int32_t)(window < kMaxPositions ? window : kMaxPositions);
     a.shared = blocks;
+    a.waves = paged_waves(sequences, heads, kv_heads, longest);
     a.workspace = static_cast<float*>(workspace);
     return from_hip(launch_paged_attention(a, stream));
 }

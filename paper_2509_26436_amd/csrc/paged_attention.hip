@@ -28,8 +28,8 @@
 // waves' sums meet in shared memory.  A head that lies within one block's run is
 // finished there; of the others each block leaves (maximum, sum, O) in the
 // workspace, at most two such parts a block, and a second kernel joins them.
-// Where the table is narrow every head is one block's, and there is no second
-// kernel.
+// Where the table is narrow a block takes a head, with as many waves as have keys
+// to read, and there is no second kernel.
 #include <algorithm>
 
 #include "quartz_internal.h"
@@ -431,21 +431,13 @@ __global__ __launch_bounds__(64 * WAVES, SHARED ? fits(D, FP8) : 1) void paged_a
     if constexpr (SHARED) {
         key0 = at.range.from + at.unit * kUnit + kStep * wave;
         begin(at);
-    } else if (a.window == 0) {
-        // no need to know the length for the first step: the table has entries
-        // there, and a page is read whatever it holds
-        key0 = kStep * wave;
-        if (c.table_pages > 0)
-            begin(at);
-        at.range = key_range(a, at.b, kUnit);
     } else {
         at.range = key_range(a, at.b, kUnit);
+        at.count = at.range.units;
         key0 = at.range.from + kStep * wave;
-        if (c.table_pages > 0)
+        if (key0 < at.range.n)
             begin(at);
     }
-    if constexpr (!SHARED)
-        at.count = at.range.units;
 
     for (int64_t left = share.count;;) {
         end = min(at.range.n, at.range.from + (at.unit + at.count) * kUnit);
@@ -491,7 +483,9 @@ __global__ __launch_bounds__(64 * WAVES, SHARED ? fits(D, FP8) : 1) void paged_a
 
         const int kv = done.part / tiles, tile = done.part - kv * tiles;
         const int queries = min(16, group - 16 * tile), head0 = kv * group + 16 * tile;
-        if (m < queries) {
+        // a short sequence may leave waves without keys
+        const int used = SHARED ? kWaves : max(1, min(kWaves, (at.range.n - at.range.from + kStep - 1) / kStep));
+        if (m < queries && wave < used) {
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -510,11 +504,13 @@ __global__ __launch_bounds__(64 * WAVES, SHARED ? fits(D, FP8) : 1) void paged_a
             float high = part_m[0][query];
 #pragma unroll
             for (int w = 1; w < kWaves; ++w)
-                high = fmaxf(high, part_m[w][query]);
+                high = w < used ? fmaxf(high, part_m[w][query]) : high;
             v4f o = {};
             float l = 0.0f;
 #pragma unroll
             for (int w = 0; w < kWaves; ++w) {
+                if (w >= used)
+                    break;
                 const float by = __builtin_amdgcn_exp2f(part_m[w][query] - high);
                 o += *reinterpret_cast<const v4f*>(&part_o[w][query][channel]) * by;
                 l += part_l[w][query] * by;
@@ -602,11 +598,20 @@ hipError_t launch(const PagedAttention& a, hipStream_t stream)
 {
     const int tiles = tiles_of(a.heads, a.cache.heads);
     if (a.shared == 0) {
-        const uint32_t grid = (uint32_t)(a.cache.sequences * a.cache.heads * tiles);
-        if (a.cache.fp8)
-            paged_attention_kernel<D, true, 8, false><<<grid, 512, 0, stream>>>(a, tiles);
+        const auto go = [&](auto waves) {
+            constexpr int W = decltype(waves)::value;
+            const uint32_t grid = (uint32_t)(a.cache.sequences * a.cache.heads * tiles);
+            if (a.cache.fp8)
+                paged_attention_kernel<D, true, W, false><<<grid, 64 * W, 0, stream>>>(a, tiles);
+            else
+                paged_attention_kernel<D, false, W, false><<<grid, 64 * W, 0, stream>>>(a, tiles);
+        };
+        if (a.waves == 1)
+            go(std::integral_constant<int, 1>());
+        else if (a.waves == 2)
+            go(std::integral_constant<int, 2>());
         else
-            paged_attention_kernel<D, false, D == 256 ? 4 : 8, false><<<grid, D == 256 ? 256 : 512, 0, stream>>>(a, tiles);
+            go(std::integral_constant<int, 4>());
         return hipGetLastError();
     }
     if (a.cache.fp8)
@@ -630,12 +635,25 @@ int paged_blocks(int64_t sequences, int64_t heads, int64_t kv_heads, int64_t d, 
     const int64_t resident = compute_units * (4 * parts <= compute_units ? 1 : fits((int)d, fp8));
     // a window's first key may lie inside a tile
     const int64_t units = (longest + kKeys - 1 + unit_keys((int)d, fp8) - 1) / unit_keys((int)d, fp8);
-    // A block a head: one launch, and up to two passes (four) of its eight waves.
-    // 32 heads of up to 333 keys: 7.6 us against 9.0 shared; 4 x 8 heads of 1000
-    // keys: 16.9 against 9.9, but 64 x 8 of up to 1000 (e4m3) 23.6 against 25.8.
-    if (longest <= 512 || (longest <= 1024 && parts >= compute_units))
+    // A block a head (one launch) where that is at most 4 passes of its waves, or 8
+    // with a head for every compute unit.  32 heads of 512 e4m3 keys (2 passes):
+    // 7.1 us against 9.9 shared; of 1000 bf16 keys (8) 16.7 and 10.0; 512 heads of
+    // 100 to 1000 e4m3 keys 20.1 and 25.7, to 2000 (8) 35.1 and 36.0, bf16 (16) 62.1
+    // and 51.6.
+    const int64_t passes = (longest + unit_keys((int)d, fp8) - 1) / unit_keys((int)d, fp8);
+    if (passes <= 4 || (passes <= 8 && parts >= compute_units))
         return 0;
     return (int)std::min(resident, parts * units);
+}
+
+// Four, or where there are few keys as many as have some to read: 1976 heads of
+// up to 128 e4m3 keys 10.3 us with one, 12.7 with two, 17.0 with four; 32 heads of
+// 120 bf16 keys 5.7, 4.7 and 4.8.  (Eight, of 333 keys, take what four do.)
+int paged_waves(int64_t sequences, int64_t heads, int64_t kv_heads, int64_t longest)
+{
+    if (longest > 128)
+        return 4;
+    return sequences * kv_heads * tiles_of(heads, kv_heads) > device_compute_units() ? 1 : 2;
 }
 
 size_t paged_attention_bytes(int64_t d, int blocks)

@@ -348,11 +348,14 @@ struct PagedAttention {
     float scale;
     int32_t window;           // 0: all keys
     int32_t shared;           // paged_blocks
+    int32_t waves;            // paged_waves
     float* workspace;         // paged_attention_bytes
 };
 // Blocks that share the work of a call in equal runs and leave what has to be
 // joined in the workspace (on the current device); 0: a block takes a head.
 int paged_blocks(int64_t sequences, int64_t heads, int64_t kv_heads, int64_t d, bool fp8, int64_t longest);
+// waves of a block that takes a head: 1, 2 or 4
+int paged_waves(int64_t sequences, int64_t heads, int64_t kv_heads, int64_t longest);
 size_t paged_attention_bytes(int64_t d, int blocks);
 hipError_t launch_paged_attention(const PagedAttention& a, hipStream_t stream);
 

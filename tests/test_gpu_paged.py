@@ -115,6 +115,20 @@ def test_many_short_heads(kv, group, d, fp8):
     _check(R.host(o), x, R.host(k), R.host(v), table, lengths, 16)
 
 
+@pytest.mark.parametrize("S,kv", [(3, 2), (90, 6)])
+@pytest.mark.parametrize("group,d,fp8", [(4, 128, False), (19, 64, True), (1, 256, False), (2, 256, True)])
+@pytest.mark.parametrize("longest,window", [(1, 0), (33, 0), (128, 0), (90, 20), (700, 40), (250, 0)])
+def test_short_sequences(S, kv, group, d, fp8, longest, window):
+    """Blocks of one, two and four waves, some of them without keys; few heads and many."""
+    import paper_2509_26436_amd as q
+    print(f"paged attention {S} x {kv} x {group} x {d} fp8 {fp8}, up to {longest}, window {window}", flush=True)
+    lengths = _rng(17, S, longest).integers(0, longest + 1, S).tolist()
+    lengths[:2] = [longest, 0]
+    _, table, k, v, x, cache = _attention_case(18, lengths, kv, group, d, 16, fp8)
+    o = q.paged_attention(R.device(x), cache, _int32(lengths), window=window)
+    _check(R.host(o), x, R.host(k), R.host(v), table, lengths, 16, window=window)
+
+
 @pytest.mark.parametrize("window", [1, 7, 32, 100, 5000])
 @pytest.mark.parametrize("fp8", [False, True])
 def test_window_and_scale(window, fp8):
