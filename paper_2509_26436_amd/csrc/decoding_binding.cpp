@@ -95,7 +95,7 @@ void* address(const Tensor& t) { return t.defined() ? t.data_ptr() : nullptr; }
 template <typename... T>
 void same_device(const Tensor& a, const T&... others)
 {
-    auto check = [&](const Tensor& t) {
+    [[maybe_unused]] auto check = [&](const Tensor& t) {
         NEED(!t.defined() || t.device() == a.device(), "all tensors must be on one device: ", t.device(), " beside ",
              a.device());
     };
