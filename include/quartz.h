@@ -675,7 +675,8 @@ quartz_status quartz_rotary(const void* x_bf16, void* y_bf16, int64_t tokens, in
  *              needed) on the current device, any contents.  Calls that share one
  *              must not overlap in time.
  * The host reads no lengths (the kernels share the work by them): a call may be
- * captured into a graph and replayed with other lengths, pages and tokens.
+ * captured into a graph and replayed with other lengths, pages and tokens, which
+ * must stay as they are while it runs.
  */
 enum { QUARTZ_CACHE_BF16 = 0, QUARTZ_CACHE_E4M3 = 1 };
 
