@@ -643,8 +643,9 @@ quartz_status quartz_rotary(const void* x_bf16, void* y_bf16, int64_t tokens, in
 /*
  * Paged cache of one layer's keys and values:
  *   k_cache, v_cache  [pages][heads][page_size][d] of bf16 (QUARTZ_CACHE_BF16) or
- *              OCP e4m3 (QUARTZ_CACHE_E4M3), page_stride elements from a page to
- *              the next (at least heads page_size d; a multiple of 16 bytes).  A
+ *              OCP e4m3 (QUARTZ_CACHE_E4M3), at least one page, page_stride elements
+ *              from one to the next (heads page_size d or more; a multiple of 16
+ *              bytes).  A
  *              stored value stands for itself times k_scale (v_scale), positive
  *              and normal.  d is 64, 128 or 256, page_size a power of two from 8
  *              to 4096.
