@@ -44,11 +44,13 @@ typedef float v4f __attribute__((ext_vector_type(4)));
 typedef uint32_t v4u __attribute__((ext_vector_type(4)));
 
 constexpr int kKeys = 32;                        // keys of a matrix tile
-// Tiles of a wave's step: as many as make its loads 16 KB (8 KB for e4m3 of 64
-// channels), which keeps the memory busy with the waves that fit.
-constexpr int step_tiles(int d, bool fp8) { return d == 64 || (d == 128 && fp8) ? 2 : 1; }
+// Tiles of a wave's step.  In a block that takes a head as many as make its loads
+// 16 KB (8 KB for e4m3 of 64 channels); where blocks share the keys one, which
+// lets more of them fit a compute unit and wastes less at a head's end (512 heads of
+// 129 to 4096 e4m3 keys: 54.3 us, with two tiles 59.0).
+constexpr int step_tiles(int d, bool fp8, bool shared) { return !shared && (d == 64 || (d == 128 && fp8)) ? 2 : 1; }
 // keys of a unit of work: a step of four waves
-constexpr int unit_keys(int d, bool fp8) { return 4 * kKeys * step_tiles(d, fp8); }
+constexpr int unit_keys(int d, bool fp8, bool shared) { return 4 * kKeys * step_tiles(d, fp8, shared); }
 constexpr float kNoScore = -3.0e38f;             // a maximum below every score that counts
 
 // N words that are read once (16-byte loads around the caches' replacement
@@ -156,8 +158,8 @@ struct Head {
     KeyRange range;
 };
 
-// waves a block may use, and blocks of four waves that fit a compute unit
-constexpr int fits(int d, bool fp8) { return d == 64 ? 3 : d == 128 ? (fp8 ? 2 : 3) : 1; }
+// shared blocks, of four waves, that fit a compute unit
+constexpr int fits(int d, bool fp8) { return d <= 128 ? 3 : fp8 ? 2 : 1; }
 
 // SHARED: a block takes a run of units; otherwise a head.
 template <int D, bool FP8, int WAVES, bool SHARED>
@@ -165,7 +167,8 @@ __global__ __launch_bounds__(64 * WAVES, SHARED ? fits(D, FP8) : 1) void paged_a
     const PagedAttention a, int tiles)
 {
     constexpr int kWaves = WAVES, kThreads = 64 * kWaves;
-    constexpr int kR = step_tiles(D, FP8), kStep = kKeys * kR, kPass = kStep * kWaves, kUnit = unit_keys(D, FP8);
+    constexpr int kR = step_tiles(D, FP8, SHARED), kStep = kKeys * kR, kPass = kStep * kWaves;
+    constexpr int kUnit = unit_keys(D, FP8, SHARED);
     constexpr int kSteps = D / 32;               // matrix steps over the channels
     constexpr int kTiles = D / 16;               // row tiles of O^T
     constexpr int kRun = FP8 || D < 256 ? kTiles : 8;        // channels of a lane's load of V: at most 16 bytes
@@ -630,17 +633,17 @@ int paged_blocks(int64_t sequences, int64_t heads, int64_t kv_heads, int64_t d, 
     // Few heads: a block a compute unit, whose long runs one after the other the
     // memory serves best (8 heads of 262143 keys: 162 us, with three 173).  Many:
     // as many as fit, so that one's change of heads is another's work (512 heads
-    // of 129 to 4096 e4m3 keys: 70 us with one, 59 with two).
+    // of 129 to 4096 e4m3 keys: 63 us with one, 54 with three).
     const int64_t compute_units = device_compute_units();
     const int64_t resident = compute_units * (4 * parts <= compute_units ? 1 : fits((int)d, fp8));
     // a window's first key may lie inside a tile
-    const int64_t units = (longest + kKeys - 1 + unit_keys((int)d, fp8) - 1) / unit_keys((int)d, fp8);
+    const int64_t unit = unit_keys((int)d, fp8, true), units = (longest + kKeys - 1 + unit - 1) / unit;
     // A block a head (one launch) where that is at most 4 passes of its waves, or 8
     // with a head for every compute unit.  32 heads of 512 e4m3 keys (2 passes):
     // 7.1 us against 9.9 shared; of 1000 bf16 keys (8) 16.7 and 10.0; 512 heads of
     // 100 to 1000 e4m3 keys 20.1 and 25.7, to 2000 (8) 35.1 and 36.0, bf16 (16) 62.1
     // and 51.6.
-    const int64_t passes = (longest + unit_keys((int)d, fp8) - 1) / unit_keys((int)d, fp8);
+    const int64_t pass = unit_keys((int)d, fp8, false), passes = (longest + pass - 1) / pass;
     if (passes <= 4 || (passes <= 8 && parts >= compute_units))
         return 0;
     return (int)std::min(resident, parts * units);
