@@ -640,9 +640,10 @@ int paged_blocks(int64_t sequences, int64_t heads, int64_t kv_heads, int64_t d, 
     const int64_t unit = unit_keys((int)d, fp8, true), units = (longest + kKeys - 1 + unit - 1) / unit;
     // A block a head (one launch) where that is at most 4 passes of its waves, or 8
     // with a head for every compute unit.  32 heads of 512 e4m3 keys (2 passes):
-    // 7.1 us against 9.9 shared; of 1000 bf16 keys (8) 16.7 and 10.0; 512 heads of
-    // 100 to 1000 e4m3 keys 20.1 and 25.7, to 2000 (8) 35.1 and 36.0, bf16 (16) 62.1
-    // and 51.6.
+    // 7.1 us against 9.3 shared; of 1000 bf16 keys (8) 12.8 and 10.0; 512 heads of
+    // 100 to 1000 e4m3 keys (4) 21.2 and 22.5, of 1900 to 2000 (8) 45.9 and 49.5
+    // (of 100 to 2000, uneven, 36.4 and 32.3), of 100 to 2000 bf16 keys (16) 62.6
+    // and 51.4.
     const int64_t pass = unit_keys((int)d, fp8, false), passes = (longest + pass - 1) / pass;
     if (passes <= 4 || (passes <= 8 && parts >= compute_units))
         return 0;
