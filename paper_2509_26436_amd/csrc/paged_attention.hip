@@ -15,9 +15,11 @@
 //     registers; row m of tile t is channel t of lane m's run, so that at the end
 //     a lane holds neighbouring channels of its query.
 // The softmax runs over the pass with a running maximum and sum in fp32 (base-2
-// exponentials).  P is rounded to bf16 for the product, with a relative error of
-// up to 2^-8 a weight as for the output itself, and the sum is that of the
-// rounded weights (a row of ones beside V), so that weights add up to one.
+// exponentials).  P goes into the product as two bf16 parts, its rounding and the
+// rest of it (a relative error of up to 2^-16 a weight, where one part would leave
+// 2^-8), and the sum is that of the same parts (a row of ones beside V), so that
+// weights add up to one.  The memory still bounds the call: 512 heads of 129 to
+// 4096 e4m3 keys take 51.6 us with both parts and 51.1 with one.
 // e4m3 keys and values are expanded to bf16, exactly, after the load; their
 // scales go into the softmax scale and the output.
 //
@@ -382,10 +384,16 @@ __global__ __launch_bounds__(64 * WAVES, SHARED ? fits(D, FP8) : 1) void paged_a
 #pragma unroll
             for (int j = 0; j < 8; ++j)
                 p[r][j] = __builtin_amdgcn_exp2f(p[r][j] - top);
-            const v4u pf = {pack_bf16(p[r][0], p[r][1]), pack_bf16(p[r][2], p[r][3]), pack_bf16(p[r][4], p[r][5]),
-                            pack_bf16(p[r][6], p[r][7])};
+            v4u pf, rest;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float a = p[r][2 * j], b = p[r][2 * j + 1];
+                pf[j] = pack_bf16(a, b);
+                rest[j] = pack_bf16(a - __uint_as_float(pf[j] << 16), b - __uint_as_float(pf[j] & 0xFFFF0000u));
+            }
             const uint32_t one = 0x3F803F80u;
-            sum = mfma(v4u{one, one, one, one}, pf, sum);
+            const v4u ones = {one, one, one, one};
+            sum = mfma(ones, rest, mfma(ones, pf, sum));
             // a channel's 8 keys from a word (two channels, e4m3: four) of each key's row
 #pragma unroll
             for (int t = 0; t < kTiles; ++t) {
@@ -403,7 +411,7 @@ __global__ __launch_bounds__(64 * WAVES, SHARED ? fits(D, FP8) : 1) void paged_a
                     }
                     vf[j] = __builtin_amdgcn_perm(hi, lo, pick);
                 }
-                acc[t] = mfma(vf, pf, acc[t]);
+                acc[t] = mfma(vf, rest, mfma(vf, pf, acc[t]));
             }
         }
     };

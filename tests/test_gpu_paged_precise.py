@@ -1,0 +1,58 @@
+"""Attention over the paged cache where small errors show: values that cancel under nearly equal
+weights, against the definition in 64 bits with bounds that count the steps in fp32."""
+import math
+
+import numpy as np
+import pytest
+
+import decoding_reference as R
+import test_gpu_paged as P
+
+pytestmark = pytest.mark.gpu
+
+
+def _bounds(q, k, v, scale):
+    """One sequence and cache head: (o, how far it may be) with weights that hold 16 bits or more."""
+    n, d = k.shape
+    s = scale * (q @ k.T)
+    size = abs(scale) * (np.abs(q) @ np.abs(k).T)
+    p = np.exp(s - s.max(-1, keepdims=True))
+    p /= p.sum(-1, keepdims=True)
+    o, weight = p @ v, p @ np.abs(v)
+    # the score's additions and three roundings; the exponent's argument, up to 128 in base 2, rounded
+    # once more; a weight's own rounding to two bf16 parts (2^-16) in the product and in the sum; the
+    # additions of n weighted values and of n weights
+    off = ((d + 8) * R.ADD * size + 4 * 2.0 ** -24 * (np.abs(s) + 1)).max(-1, keepdims=True)
+    far = weight * (2 * np.expm1(off) + 2 * 2.0 ** -16 + 2.0 ** -20 + 2 * (2 * n + 8) * R.ADD)
+    return o, R.HALF_BF16 * np.abs(o) + (1 + R.HALF_BF16) * far + 1e-37
+
+
+@pytest.mark.parametrize("width", [None, 4096])
+@pytest.mark.parametrize("kv,group,d,fp8", [(2, 4, 128, False), (2, 4, 128, True), (1, 3, 64, False),
+                                            (3, 1, 64, True), (1, 20, 256, False), (1, 2, 256, True)])
+def test_weights_of_cancelling_values(kv, group, d, fp8, width):
+    """Neighbouring keys hold a value and its negative under weights that differ a little: what is
+    left is the weights' difference, which a weight rounded to bf16 (off by up to 2^-8) would lose."""
+    import torch
+    import paper_2509_26436_amd as q
+    print(f"weights: {kv} x {group} x {d} fp8 {fp8} width {width}", flush=True)
+    page, lengths = 16, [2, 300, 64, 500]
+    rng, table, k, v, x, cache = P._attention_case(21, lengths, kv, group, d, page, fp8,
+                                                   width=None if width is None else width // page)
+    kh, vh = R.host(k), R.host(v)
+    kh[..., 1:] = 0.0                      # one channel scores: its products are exact
+    vh[:, :, 1::2] = -vh[:, :, ::2]
+    for t, h in ((k, kh), (v, vh)):
+        t.copy_(torch.from_numpy(h).cuda().to(torch.bfloat16).to(t.dtype))
+    x[:, :, 0] = R.bf16(rng.uniform(0.3, 1.0, x.shape[:2]))
+    scale = 0.25
+    assert (q.paged_attention_workspace(len(lengths), kv * group, cache) is not None) == (width is not None)
+    o = R.host(q.paged_attention(R.device(x), cache, P._int32(lengths), scale=scale))
+    kh, vh = R.host(k), R.host(v)
+    for b, n in enumerate(lengths):
+        for h in range(kv):
+            kk, vv = (P._gather(t, table, b, h, n, page) for t in (kh, vh))
+            rows = slice(h * group, (h + 1) * group)
+            want, far = _bounds(x[b, rows], kk, vv, scale)
+            off = np.abs(o[b, rows] - want)
+            assert (off <= far).all(), (b, h, n, (off / far).max())
