@@ -23,6 +23,8 @@ constexpr int64_t kMaxAppend = int64_t(1) << 31;
 // positions of one sequence's pages
 constexpr int64_t kMaxPositions = int64_t(1) << 30;
 constexpr int64_t kMaxStride = int64_t(1) << 40;
+// attention's v_scale: over a sum of weights of up to kMaxPositions still normal
+constexpr float kMinValueScale = 0x1p-96f;
 
 bool layout_ok(int32_t layout) { return layout == QUARTZ_ROTARY_HALF || layout == QUARTZ_ROTARY_INTERLEAVED; }
 
@@ -343,7 +345,9 @@ quartz_status quartz_paged_attention(const void* q_bf16, void* o_bf16, int64_t s
                                      float scale, int64_t window, void* workspace, size_t workspace_bytes,
                                      hipStream_t stream)
 {
-    if (!std::isfinite(scale))
+    // one factor for the scores, which fp32 has to hold with all its bits
+    const double factor = (double)scale * (double)k_scale * 1.4426950408889634;
+    if (!std::isfinite(scale) || (factor != 0.0 && !std::isnormal((float)factor)) || v_scale < kMinValueScale)
         return QUARTZ_ERR_UNSUPPORTED;
     int64_t longest = 0;
     quartz_status st = attention_checks(sequences, heads, kv_heads, d, page_size, table_pages, window, longest);
@@ -375,7 +379,7 @@ quartz_status quartz_paged_attention(const void* q_bf16, void* o_bf16, int64_t s
     a.o_head = o_head;
     a.heads = (int32_t)heads;
     a.lengths = lengths;
-    a.scale = scale;
+    a.scale = (float)factor;
     a.window = (int32_t)(window < kMaxPositions ? window : kMaxPositions);
     a.shared = blocks;
     a.waves = paged_waves(sequences, heads, kv_heads, longest);

@@ -258,7 +258,6 @@ __global__ __launch_bounds__(64 * WAVES, SHARED ? fits(D, FP8) : 1) void paged_a
     }
 
     // the head in work: its pointers, Q^T, sums, and the first step's keys and values
-    const float scale = a.scale * 1.4426950408889634f * c.k_scale;
     const int mask = (1 << c.page_shift) - 1, last_page = c.table_pages - 1;
     const uint8_t *keys, *values;
     const int32_t* table;
@@ -338,8 +337,8 @@ __global__ __launch_bounds__(64 * WAVES, SHARED ? fits(D, FP8) : 1) void paged_a
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                p[r][i] = s0[i] * scale;
-                p[r][4 + i] = s1[i] * scale;
+                p[r][i] = s0[i] * a.scale;
+                p[r][4 + i] = s1[i] * a.scale;
             }
         }
     };
@@ -527,7 +526,7 @@ __global__ __launch_bounds__(64 * WAVES, SHARED ? fits(D, FP8) : 1) void paged_a
                 l += part_l[w][query] * by;
             }
             if (whole) {
-                const float by = l == 0.0f ? 0.0f : c.v_scale / l;
+                const float by = l == 0.0f ? 0.0f : c.v_scale / l;     // normal: v_scale is at least 2^-96
                 *reinterpret_cast<uint2*>(a.o + done.b * a.o_token + (head0 + query) * a.o_head + channel) =
                     uint2{pack_bf16(o[0] * by, o[1] * by), pack_bf16(o[2] * by, o[3] * by)};
             } else {

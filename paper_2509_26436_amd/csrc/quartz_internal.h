@@ -345,7 +345,7 @@ struct PagedAttention {
     int64_t q_token, q_head, o_token, o_head;
     int32_t heads;            // of q: a multiple of cache.heads
     const int32_t* lengths;
-    float scale;
+    float scale;              // of q . k to scores in units of log2, the cache's k_scale in it
     int32_t window;           // 0: all keys
     int32_t shared;           // paged_blocks
     int32_t waves;            // paged_waves
