@@ -668,9 +668,9 @@ quartz_status quartz_rotary(const void* x_bf16, void* y_bf16, int64_t tokens, in
  * (window > 0); query head h reads cache head h / (heads / kv_heads).  lengths
  * are clamped to [0, table_pages page_size]; positions without a page have no
  * weight, and what the cache holds in places that do not count (infinities and
- * NaN too) does not matter.  Without any key the output is 0.  Scores and sums are
-fp32: scale k_scale log2(e) has to be 0 or a normal fp32 number, and v_scale at
-least 2^-96 (QUARTZ_ERR_UNSUPPORTED otherwise).
+ * NaN too) does not matter.  Without any key, or if every score is -inf, the output
+ * is 0.  Scores and sums are fp32: scale k_scale log2(e) has to be 0 or a normal
+ * fp32 number, and v_scale at least 2^-96 (QUARTZ_ERR_UNSUPPORTED otherwise).
  *   q, o       bf16 [sequences][heads][d], strides in elements: multiples of 8
  *              for q, of 4 for o (whose pointer needs 8-byte alignment).
  *   table      row b belongs to sequence b (rows = sequences).

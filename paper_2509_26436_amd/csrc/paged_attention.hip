@@ -33,6 +33,7 @@
 // Where the table is narrow a block takes a head, with as many waves as have keys
 // to read, and there is no second kernel.
 #include <algorithm>
+#include <cfloat>
 
 #include "quartz_internal.h"
 
@@ -53,7 +54,9 @@ constexpr int kKeys = 32;                        // keys of a matrix tile
 constexpr int step_tiles(int d, bool fp8, bool shared) { return !shared && (d == 64 || (d == 128 && fp8)) ? 2 : 1; }
 // keys of a unit of work: a step of four waves
 constexpr int unit_keys(int d, bool fp8, bool shared) { return 4 * kKeys * step_tiles(d, fp8, shared); }
-constexpr float kNoScore = -3.0e38f;             // a maximum below every score that counts
+// A maximum no score is below.  Finite, so that parts without keys join without
+// inf - inf; only keys of score -inf have no weight against it.
+constexpr float kNoScore = -FLT_MAX;
 
 // N words that are read once (16-byte loads around the caches' replacement
 // reach 7.1 TB/s where ordinary ones reach 6.2)

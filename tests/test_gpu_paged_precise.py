@@ -108,3 +108,29 @@ def test_a_small_scale_over_many_keys(kv):
     o = q.paged_attention(x, cache, P._int32([n]))
     want = R.host(values) * v_scale
     np.testing.assert_array_equal(R.host(o), np.broadcast_to(want, (1, kv, d)))
+
+
+@pytest.mark.parametrize("width", [None, 4096])
+@pytest.mark.parametrize("lengths", [[1, 40, 0], [128, 7, 500]])
+def test_the_lowest_scores(lengths, width):
+    """Scores beside fp32's lowest number still count: equal ones average the values.  (In units of
+    log2, which the kernel's scores have, -1.25 2^127 is -3.07e38.)  Scores of -inf alone give 0."""
+    import torch
+    import paper_2509_26436_amd as q
+    page, d, kv = 16, 64, 2
+    _, table, k, v, x, cache = P._attention_case(23, lengths, kv, 1, d, page, False,
+                                                 width=None if width is None else width // page)
+    k.zero_()
+    k[:, 0, :, 5], k[:, 1, :, 5] = -1.25 * 2.0 ** 64, -math.inf
+    x = np.zeros_like(x)
+    x[..., 5] = 2.0 ** 63
+    o = R.host(q.paged_attention(R.device(x), cache, P._int32(lengths), scale=1.0))
+    vh = R.host(v)
+    for b, n in enumerate(lengths):
+        assert (o[b, 1] == 0).all()
+        if n == 0:
+            assert (o[b, 0] == 0).all()
+            continue
+        vv = P._gather(vh, table, b, 0, n, page)
+        want, far = _bounds(np.zeros((1, d)), np.zeros((n, d)), vv, 1.0)          # equal weights
+        assert (np.abs(o[b, 0] - want[0]) <= far[0]).all(), (b, n)
