@@ -69,6 +69,7 @@ int32_t layout_of(PyObject* o)
 // strides count where more than one element is reached
 bool strided(const Tensor& t, int64_t dim) { return t.size(dim) > 1 && t.numel() > 0; }
 bool unit(const Tensor& t, int64_t dim) { return !strided(t, dim) || t.stride(dim) == 1; }
+int64_t stride_of(const Tensor& t, int64_t dim) { return strided(t, dim) ? t.stride(dim) : 0; }
 
 // an output whose elements are distinct, and (where that can be seen) none of them an input's
 template <typename... T>
@@ -87,7 +88,12 @@ void fresh(const Tensor& out, const T&... inputs)
 
 bool in_place(const Tensor& out, const Tensor& x)
 {
-    return out.defined() && out.data_ptr() == x.data_ptr() && out.sizes() == x.sizes() && out.strides() == x.strides();
+    if (!out.defined() || out.data_ptr() != x.data_ptr() || out.sizes() != x.sizes())
+        return false;
+    for (int64_t i = 0; i < x.dim(); ++i)
+        if (stride_of(out, i) != stride_of(x, i))
+            return false;
+    return true;
 }
 
 void* address(const Tensor& t) { return t.defined() ? t.data_ptr() : nullptr; }
@@ -346,9 +352,9 @@ PyObject* rotary(PyObject*, PyObject* const* a, Py_ssize_t n)
     heads_of(out, "out");
     NEED(out.sizes() == x.sizes(), "out must have x's shape");
     launch("quartz_rotary", x, [&](hipStream_t s) {
-        return quartz_rotary(x.data_ptr(), out.data_ptr(), tokens, heads, d, rot, x.stride(0), x.stride(1),
-                             out.stride(0), out.stride(1), p, static_cast<const int64_t*>(freqs.data_ptr()), layout,
-                             inverse, magnitude, s);
+        return quartz_rotary(x.data_ptr(), out.data_ptr(), tokens, heads, d, rot, stride_of(x, 0), stride_of(x, 1),
+                             stride_of(out, 0), stride_of(out, 1), p,
+                             static_cast<const int64_t*>(freqs.data_ptr()), layout, inverse, magnitude, s);
     });
     return THPVariable_Wrap(std::move(out));
     END_HANDLE_TH_ERRORS
@@ -423,10 +429,10 @@ PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n)
     const float magnitude = (float)real(a[11]);
     same_device(c.k, k, v, positions, sequences, freqs);
     launch("quartz_paged_append", k, [&](hipStream_t stream) {
-        return quartz_paged_append(k.data_ptr(), v.data_ptr(), tokens, c.heads, c.d, k.stride(0), k.stride(1),
-                                   v.stride(0), v.stride(1), p, s, static_cast<const int64_t*>(address(freqs)), rot,
-                                   layout, magnitude, c.k.data_ptr(), c.v.data_ptr(), c.type, c.k_scale, c.v_scale,
-                                   c.pages, c.page, c.stride, table_at(c), c.table.size(0), c.table.size(1),
+        return quartz_paged_append(k.data_ptr(), v.data_ptr(), tokens, c.heads, c.d, stride_of(k, 0),
+                                   stride_of(k, 1), stride_of(v, 0), stride_of(v, 1), p, s,
+                                   static_cast<const int64_t*>(address(freqs)), rot, layout, magnitude,
+                                   c.k.data_ptr(), c.v.data_ptr(), c.type, c.k_scale, c.v_scale, c.pages, c.page, c.stride, table_at(c), c.table.size(0), c.table.size(1),
                                    table_stride(c), stream);
     });
     Py_RETURN_NONE;
@@ -459,9 +465,9 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n)
         workspace, quartz_paged_attention_workspace_bytes(sequences, heads, c.heads, d, c.page, c.table.size(1), window),
         q);
     launch("quartz_paged_attention", q, [&](hipStream_t s) {
-        return quartz_paged_attention(q.data_ptr(), out.data_ptr(), sequences, heads, c.heads, d, q.stride(0),
-                                      q.stride(1), out.stride(0), out.stride(1), c.k.data_ptr(), c.v.data_ptr(),
-                                      c.type, c.k_scale, c.v_scale, c.pages, c.page, c.stride, table_at(c),
+        return quartz_paged_attention(q.data_ptr(), out.data_ptr(), sequences, heads, c.heads, d, stride_of(q, 0),
+                                      stride_of(q, 1), stride_of(out, 0), stride_of(out, 1), c.k.data_ptr(),
+                                      c.v.data_ptr(), c.type, c.k_scale, c.v_scale, c.pages, c.page, c.stride, table_at(c),
                                       c.table.size(1), table_stride(c), len, scale, window, address(workspace), size,
                                       s);
     });
