@@ -6,12 +6,12 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
-#include <ATen/MemoryOverlap.h>
 #include <c10/hip/HIPGuard.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <algorithm>
 #include <cmath>
 
 #include "quartz.h"
@@ -71,19 +71,129 @@ bool strided(const Tensor& t, int64_t dim) { return t.size(dim) > 1 && t.numel()
 bool unit(const Tensor& t, int64_t dim) { return !strided(t, dim) || t.stride(dim) == 1; }
 int64_t stride_of(const Tensor& t, int64_t dim) { return strided(t, dim) ? t.stride(dim) : 0; }
 
-// an output whose elements are distinct, and (where that can be seen) none of them an input's
+// Whether sum c_k w_k = target has a solution with 0 <= c_k <= most_k: the places
+// that a strided tensor reaches, or the differences of two tensors' places.  The
+// largest weight goes first: what the others reach in all leaves it few values, one
+// or two where strides nest as they do in views of one tensor.
+class Combination {
+public:
+    void add(int64_t weight, int64_t most)
+    {
+        if (most <= 0)
+            return;
+        int i = 0;
+        while (i < count_ && weight_[i] > weight)
+            ++i;
+        if (i < count_ && weight_[i] == weight) {
+            most_[i] += most;
+            return;
+        }
+        NEED(count_ < kTerms, "tensors of that many dimensions cannot be told apart");
+        for (int j = count_++; j > i; --j) {
+            weight_[j] = weight_[j - 1];
+            most_[j] = most_[j - 1];
+        }
+        weight_[i] = weight;
+        most_[i] = most;
+    }
+
+    bool reaches(int64_t target)
+    {
+        reach_[count_] = 0;
+        dense_[count_] = true;
+        for (int k = count_ - 1; k >= 0; --k) {
+            reach_[k] = reach_[k + 1] + weight_[k] * most_[k];
+            dense_[k] = dense_[k + 1] && weight_[k] <= reach_[k + 1] + 1;
+        }
+        tries_ = 0;
+        return search(0, target);
+    }
+
+private:
+    bool search(int k, int64_t target)
+    {
+        if (target < 0 || target > reach_[k])
+            return false;
+        if (dense_[k])                             // every number up to there
+            return true;
+        NEED(++tries_ <= kTries, "tensors of these strides cannot be told apart");
+        const int64_t rest = target - reach_[k + 1];
+        int64_t c = rest > 0 ? (rest + weight_[k] - 1) / weight_[k] : 0;
+        for (const int64_t last = std::min(most_[k], target / weight_[k]); c <= last; ++c)
+            if (search(k + 1, target - c * weight_[k]))
+                return true;
+        return false;
+    }
+
+    static constexpr int kTerms = 16, kTries = 100000;
+    int64_t weight_[kTerms], most_[kTerms], reach_[kTerms + 1];
+    bool dense_[kTerms + 1];
+    int count_ = 0, tries_ = 0;
+};
+
+// bytes from a tensor's first element to the end of its last
+int64_t extent(const Tensor& t)
+{
+    int64_t elements = 1;
+    for (int64_t i = 0; i < t.dim(); ++i)
+        elements += (t.size(i) - 1) * t.stride(i);
+    return elements * t.element_size();
+}
+
+// two tensors with a byte in common
+bool share(const Tensor& a, const Tensor& b)
+{
+    if (!a.defined() || !b.defined() || a.numel() == 0 || b.numel() == 0 || a.device() != b.device())
+        return false;
+    const int64_t a0 = reinterpret_cast<int64_t>(a.data_ptr()), b0 = reinterpret_cast<int64_t>(b.data_ptr());
+    const int64_t b_extent = extent(b);
+    if (a0 + extent(a) <= b0 || b0 + b_extent <= a0)
+        return false;
+    // a0 + i = b0 + j for places i of a and j of b: i + (b's extent - 1 - j) = b0 - a0 + b's extent - 1
+    Combination c;
+    c.add(1, a.element_size() - 1 + b.element_size() - 1);
+    for (const Tensor* t : {&a, &b})
+        for (int64_t i = 0; i < t->dim(); ++i)
+            if (t->stride(i) != 0)
+                c.add(t->stride(i) * t->element_size(), t->size(i) - 1);
+    return c.reaches(b0 - a0 + b_extent - 1);
+}
+
+// a tensor that reaches one element twice
+bool repeats(const Tensor& t)
+{
+    if (t.numel() == 0 || t.is_contiguous())
+        return false;
+    for (int64_t k = 0; k < t.dim(); ++k) {
+        if (t.size(k) == 1)
+            continue;
+        if (t.stride(k) == 0)
+            return true;
+        // two places apart by one step of k or more, and by any of the others' steps either way: none
+        Combination c;
+        c.add(t.stride(k), t.size(k) - 2);
+        int64_t target = -t.stride(k);
+        for (int64_t i = 0; i < t.dim(); ++i) {
+            if (i == k || t.size(i) == 1)
+                continue;
+            if (t.stride(i) != 0)
+                c.add(t.stride(i), 2 * (t.size(i) - 1));
+            target += (t.size(i) - 1) * t.stride(i);
+        }
+        if (c.reaches(target))
+            return true;
+    }
+    return false;
+}
+
+// an output whose elements are distinct, and none of them an input's
 template <typename... T>
 void fresh(const Tensor& out, const T&... inputs)
 {
     if (!out.defined())
         return;
-    NEED(at::has_internal_overlap(out) != at::MemOverlap::Yes, "out must not hold one element twice");
-    [[maybe_unused]] auto check = [&](const Tensor& t) {
-        const at::MemOverlapStatus shared = t.defined() ? at::get_overlap_status(out, t) : at::MemOverlapStatus::No;
-        NEED(shared != at::MemOverlapStatus::Full && shared != at::MemOverlapStatus::Partial,
-             "out must not share memory with an input");
-    };
-    (check(inputs), ...);
+    NEED(!repeats(out), "out must not hold one element twice");
+    NEED(!(share(out, inputs) || ...), "out must not share memory with an input");
 }
 
 bool in_place(const Tensor& out, const Tensor& x)
@@ -432,8 +542,8 @@ PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n)
         return quartz_paged_append(k.data_ptr(), v.data_ptr(), tokens, c.heads, c.d, stride_of(k, 0),
                                    stride_of(k, 1), stride_of(v, 0), stride_of(v, 1), p, s,
                                    static_cast<const int64_t*>(address(freqs)), rot, layout, magnitude,
-                                   c.k.data_ptr(), c.v.data_ptr(), c.type, c.k_scale, c.v_scale, c.pages, c.page, c.stride, table_at(c), c.table.size(0), c.table.size(1),
-                                   table_stride(c), stream);
+                                   c.k.data_ptr(), c.v.data_ptr(), c.type, c.k_scale, c.v_scale, c.pages, c.page,
+                                   c.stride, table_at(c), c.table.size(0), c.table.size(1), table_stride(c), stream);
     });
     Py_RETURN_NONE;
     END_HANDLE_TH_ERRORS

@@ -26,3 +26,84 @@ def test_attention_scales_out_of_fp32():
         assert attend(ks=ks, scale=scale) == EWS, (ks, scale)
     assert attend(vs=2.0 ** -97) == attend(vs=2.0 ** -126) == EUNSUP
     assert attend(vs=2.0 ** -96) == attend(vs=3.3e38) == EWS
+
+
+def _answer(call):
+    """What a helper says of CPU tensors: the refusal of shared memory, or (after it) of the device."""
+    with pytest.raises(ValueError) as e:
+        call()
+    for word in ("share memory", "twice", "on a GPU"):
+        if word in str(e.value):
+            return word
+    raise AssertionError(str(e.value))
+
+
+def test_outputs_that_overlap_strided_inputs():
+    """Views of one tensor that reach a common element, whatever their strides, and views side by side,
+    which do not."""
+    import torch
+    bf16 = torch.bfloat16
+    x = torch.zeros((8, 128), dtype=bf16)
+    w = q.MxTensor(torch.zeros((4, 8, 16), dtype=torch.uint8), torch.zeros((1, 8, 4), dtype=torch.uint8), 8, 128)
+    wide = torch.zeros((8, 256), dtype=bf16)
+    pos, f = torch.zeros(4, dtype=torch.int32), q.rotary_frequencies(64, device="cpu")
+    rows = torch.zeros((4, 6, 64), dtype=bf16)
+    k = torch.zeros((3, 2, 16, 64), dtype=bf16)
+    cache = q.PagedCache(k, k.clone(), torch.zeros((4, 2), dtype=torch.int32))
+    assert _answer(lambda: q.mxfp4_linear(x, w, out=x[:, :8])) == "share memory"
+    assert _answer(lambda: q.mxfp4_linear(wide[:, :128], w, out=wide[:, 120:130])) == "share memory"
+    assert _answer(lambda: q.mxfp4_linear(wide[:, :128], w, out=wide[:, 128:136])) == "on a GPU"
+    assert _answer(lambda: q.paged_attention(rows[:, :2], cache, pos, out=rows[:, 1:3])) == "share memory"
+    assert _answer(lambda: q.paged_attention(rows[:, :2], cache, pos, out=rows[:, 2:4])) == "on a GPU"
+    assert _answer(lambda: q.rotary(rows[:, :3], pos, f, out=rows[:, 3:])) == "on a GPU"
+    assert _answer(lambda: q.rotary(rows[:, :3], pos, f, out=rows[:, 2:5])) == "share memory"
+    assert _answer(lambda: q.rotary(rows[:, :3], pos, f, out=rows[:, :3])) == "on a GPU"       # in place
+    assert _answer(lambda: q.rotary(rows[:, ::2], pos, f, out=rows[:, 1::2])) == "on a GPU"
+    assert _answer(lambda: q.rotary(rows[:, :3], pos, f, out=rows.as_strided((4, 3, 64), (64, 64, 1)))) == "twice"
+    assert _answer(lambda: q.rotary(rows[:, :3], pos, f, out=torch.zeros(4 * 6 * 64 - 1, dtype=bf16).as_strided(
+        (4, 3, 64), (384, 64, 1)))) == "on a GPU"
+
+
+def test_overlaps_against_all_places():
+    """Random strided outputs in one storage: the same answer as listing every place does."""
+    import random
+    import torch
+    rng = random.Random(5)
+    base = torch.zeros(400, dtype=torch.bfloat16)
+    pos, f = torch.zeros(3, dtype=torch.int32), q.rotary_frequencies(2, device="cpu")
+
+    def view(last):
+        while True:
+            size = [rng.randint(1, 5) for _ in range(3)]
+            stride = [rng.choice([0, 1, 2, 3, 4, 5, 7, 8, 12, 20, 40]) for _ in range(3)]
+            if last:
+                size, stride = [3, *size[1:]], [*stride[:2], 1]
+            at = rng.randint(0, 100)
+            places = [at + sum(i * s for i, s in zip(index, stride)) for index in
+                      [(a, b, c) for a in range(size[0]) for b in range(size[1]) for c in range(size[2])]]
+            if max(places) < 400 and not (last and size[2] % 2):
+                return base.as_strided(size, stride, at), places
+    seen = {"share memory": 0, "twice": 0, "on a GPU": 0}
+    for _ in range(3000):
+        (x, xs), (out, outs) = view(True), view(False)
+        want = "twice" if len(set(outs)) < len(outs) else "share memory" if set(xs) & set(outs) else "on a GPU"
+        if x.data_ptr() == out.data_ptr() and x.shape == out.shape:
+            continue                                     # may be in place
+        assert _answer(lambda: q.rotary(x, pos, f, out=out)) == want, (x.shape, x.stride(), out.shape, out.stride())
+        seen[want] += 1
+    assert min(seen.values()) > 200, seen
+
+
+def test_overlaps_of_different_types():
+    """Codes of bytes and an output of 16-bit elements in one storage."""
+    import random
+    import torch
+    rng = random.Random(6)
+    raw = torch.zeros(4000, dtype=torch.uint8)
+    for _ in range(300):
+        rows, stride, at, out_at = rng.randint(1, 4), rng.choice([64, 72, 200]), rng.randint(0, 700), 2 * rng.randint(0, 700)
+        t = q.MxTensor(raw[at:at + 32 * rows].view(2, rows, 16), torch.zeros((1, rows, 4), dtype=torch.uint8), rows, 64)
+        out = raw[out_at:].view(torch.bfloat16).as_strided((rows, 24), (stride, 1))
+        places = {out_at + 2 * (r * stride + c) + b for r in range(rows) for c in range(24) for b in range(2)}
+        want = "share memory" if places & set(range(at, at + 32 * rows)) else "on a GPU"
+        assert _answer(lambda: q.mxfp4_dequantize(t, out=out)) == want
