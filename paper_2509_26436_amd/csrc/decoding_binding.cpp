@@ -196,6 +196,16 @@ void fresh(const Tensor& out, const T&... inputs)
     NEED(!(share(out, inputs) || ...), "out must not share memory with an input");
 }
 
+// a caller's workspace
+template <typename... T>
+void scratch(const Tensor& workspace, const T&... inputs)
+{
+    if (!workspace.defined())
+        return;
+    NEED(workspace.is_contiguous(), "the workspace must be contiguous");
+    NEED(!(share(workspace, inputs) || ...), "the workspace must not share memory with an input");
+}
+
 bool in_place(const Tensor& out, const Tensor& x)
 {
     if (!out.defined() || out.data_ptr() != x.data_ptr() || out.sizes() != x.sizes())
@@ -383,13 +393,11 @@ PyObject* linear_mx(PyObject*, PyObject* const* a, Py_ssize_t n)
     END_HANDLE_TH_ERRORS
 }
 
-// a workspace given by the caller, or a temporary one of `need` bytes
+// bytes of a caller's workspace, or of a temporary one of `need`
 size_t workspace_of(Tensor& workspace, size_t need, const Tensor& on)
 {
-    if (workspace.defined()) {
-        NEED(workspace.is_contiguous(), "the workspace must be contiguous");
+    if (workspace.defined())
         return workspace.nbytes();
-    }
     if (need > 0)
         workspace = at::empty({(int64_t)need}, on.options().dtype(at::kByte).requires_grad(false));
     return need;
@@ -408,6 +416,7 @@ PyObject* linear_bf16(PyObject*, PyObject* const* a, Py_ssize_t n)
     const int64_t ldx = rows_of(x, "x"), M = x.size(0);
     NEED(x.size(1) == w.K, "K mismatch between activations and weights");
     fresh(out, x, w.codes, w.scales, bias, workspace);
+    scratch(workspace, x, w.codes, w.scales, bias);
     same_device(x, w.codes, bias, out, workspace);
     const int64_t ldy = layer_out(x, M, w.rows, bias, out);
     const size_t size = workspace_of(workspace, quartz_mxfp4_linear_workspace_bytes(M, w.K), x);
@@ -565,6 +574,7 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n)
     const float scale = a[7] == Py_None ? (float)(1.0 / std::sqrt((double)d)) : (float)real(a[7]);
     Tensor out = optional(a[9], "out"), workspace = optional(a[10], "workspace");
     fresh(out, q, c.k, c.v, c.table, lengths, workspace);
+    scratch(workspace, q, c.k, c.v, c.table, lengths);
     same_device(c.k, q, lengths, out, workspace);
     const c10::hip::OptionalHIPGuard guard(q.device().index());    // the workspace is sized for its compute units
     if (!out.defined())

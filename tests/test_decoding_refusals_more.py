@@ -107,3 +107,23 @@ def test_overlaps_of_different_types():
         places = {out_at + 2 * (r * stride + c) + b for r in range(rows) for c in range(24) for b in range(2)}
         want = "share memory" if places & set(range(at, at + 32 * rows)) else "on a GPU"
         assert _answer(lambda: q.mxfp4_dequantize(t, out=out)) == want
+
+
+def test_workspaces_that_are_an_input():
+    import torch
+    bf16 = torch.bfloat16
+    x, bias = torch.zeros((40, 128), dtype=bf16), torch.zeros(2048, dtype=bf16)
+    w = q.MxTensor(torch.zeros((4, 2048, 16), dtype=torch.uint8), torch.zeros((1, 2048, 4), dtype=torch.uint8), 2048, 128)
+    for bad in (x, x[10:], w.codes, w.codes[2], w.scales, bias, x.view(torch.uint8).view(-1)[17:]):
+        assert _answer(lambda: q.mxfp4_linear(x, w, bias, workspace=bad)) == "share memory"
+        assert _answer(lambda: q.mxfp4_linear(x, w, bias, workspace=bad, out=torch.zeros((40, 2048), dtype=bf16))) == "share memory"
+    raw = torch.zeros(40 * 256 + 4096, dtype=torch.uint8)          # beside x in one storage
+    assert _answer(lambda: q.mxfp4_linear(raw[:40 * 256].view(bf16).view(40, 128), w, bias, workspace=raw[40 * 256:])) == "on a GPU"
+    with pytest.raises(ValueError, match="contiguous"):
+        q.mxfp4_linear(x, w, workspace=torch.zeros((40, 512), dtype=torch.uint8)[:, ::2])
+    rows, lengths = torch.zeros((4, 2, 64), dtype=bf16), torch.zeros(4, dtype=torch.int32)
+    k = torch.zeros((3, 2, 16, 64), dtype=bf16)
+    cache = q.PagedCache(k, k.clone(), torch.zeros((4, 400), dtype=torch.int32))
+    for bad in (rows, cache.k, cache.v[1], cache.table, lengths, cache.table[2:]):
+        assert _answer(lambda: q.paged_attention(rows, cache, lengths, workspace=bad)) == "share memory"
+    assert _answer(lambda: q.paged_attention(rows, cache, lengths, workspace=torch.zeros(9, dtype=torch.uint8))) == "on a GPU"
