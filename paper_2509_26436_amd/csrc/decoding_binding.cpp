@@ -546,6 +546,11 @@ PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n)
     const int64_t rot = freqs.defined() ? rotated(freqs, c.d) : 0;
     const int32_t layout = layout_of(a[10]);
     const float magnitude = (float)real(a[11]);
+    NEED(!share(c.k, c.v), "the cache's keys and values must not share memory");
+    for (const Tensor* pages : {&c.k, &c.v})
+        NEED(!share(*pages, k) && !share(*pages, v) && !share(*pages, positions) && !share(*pages, sequences) &&
+                 !share(*pages, freqs) && !share(*pages, c.table),
+             "the cache must not share memory with an input");
     same_device(c.k, k, v, positions, sequences, freqs);
     launch("quartz_paged_append", k, [&](hipStream_t stream) {
         return quartz_paged_append(k.data_ptr(), v.data_ptr(), tokens, c.heads, c.d, stride_of(k, 0),

@@ -127,3 +127,27 @@ def test_workspaces_that_are_an_input():
     for bad in (rows, cache.k, cache.v[1], cache.table, lengths, cache.table[2:]):
         assert _answer(lambda: q.paged_attention(rows, cache, lengths, workspace=bad)) == "share memory"
     assert _answer(lambda: q.paged_attention(rows, cache, lengths, workspace=torch.zeros(9, dtype=torch.uint8))) == "on a GPU"
+
+
+def test_append_into_its_own_inputs():
+    """A cache whose keys are its values, and new rows, positions or a table in its pages."""
+    import torch
+    bf16, i32 = torch.bfloat16, torch.int32
+    both = torch.zeros((3, 2, 2, 16, 64), dtype=bf16)
+    k, v = both[:, 0], both[:, 1]
+    table, pos, f = torch.zeros((4, 2), dtype=i32), torch.zeros(4, dtype=i32), q.rotary_frequencies(64, device="cpu")
+    rows = torch.zeros((4, 2, 64), dtype=bf16)
+    append = lambda k, v, table=table, new=(rows, rows), pos=pos, seq=None, f=f: _answer(           # noqa: E731
+        lambda: q.paged_append(q.PagedCache(k, v, table), *new, pos, seq, f))
+    assert append(k, v) == "on a GPU"                    # halves of one tensor
+    assert append(k, v, new=(both.view(-1)[:512].view(4, 2, 64), rows)) == "share memory"
+    assert append(k, v, new=(rows, v[0, :, :4].transpose(0, 1))) == "share memory"
+    assert append(k, k) == append(k, both[:, 0]) == "share memory"
+    assert append(both[:, 0], both.view(-1)[1024:1024 + 2 * 4096 + 2048].as_strided((3, 2, 16, 64), (4096, 1024, 64, 1))) == "share memory"
+    whole, v = k.contiguous(), v.contiguous()
+    words = whole.view(-1).view(i32)
+    assert append(whole, v, pos=words[:4]) == append(whole, v, seq=words[8:12]) == "share memory"
+    assert append(v, whole, table=words[:8].view(4, 2)) == "share memory"
+    assert append(whole, v, f=whole.view(-1).view(torch.int64)[:32]) == "share memory"
+    # attention reads them only
+    assert _answer(lambda: q.paged_attention(rows, q.PagedCache(whole, whole, table), pos)) == "on a GPU"
