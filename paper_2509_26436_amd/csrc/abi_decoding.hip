@@ -14,8 +14,7 @@ using namespace quartz;
 
 namespace {
 
-// blocks of 256 (512) threads whose grid stays below 2^32 threads
-constexpr int64_t kMaxBlocks256 = (int64_t(1) << 24) - 1;
+// blocks of 512 threads whose grid stays below 2^32 threads
 constexpr int64_t kMaxBlocks512 = (int64_t(1) << 23) - 1;
 // elements of one rotary (append) call: below 2^32 threads of one pair each
 constexpr int64_t kMaxRotary = int64_t(1) << 32;
@@ -275,7 +274,8 @@ quartz_status quartz_paged_append(const void* k_bf16, const void* v_bf16, int64_
         return QUARTZ_ERR_UNSUPPORTED;
     if (tokens < 0 || tokens > kMaxAppend || heads <= 0 || heads > kMaxK || d <= 0 || d > kMaxK || rot < 0 ||
         rot > d || rot % 2 != 0 || !product_ok(heads * d, tokens, kMaxAppend) || !stride_ok(k_token) ||
-        !stride_ok(k_head) || !stride_ok(v_token) || !stride_ok(v_head) || table_pages > kMaxPositions)
+        !stride_ok(k_head) || !stride_ok(v_token) || !stride_ok(v_head) || table_pages < 0 ||
+        table_pages > kMaxPositions)
         return QUARTZ_ERR_SHAPE;
     PagedAppend a{};
     a.cache = {k_cache, v_cache, pages, page_stride, (int32_t)heads, (int32_t)d, shift_of(page_size),

@@ -4,7 +4,7 @@ import os
 import pytest
 
 import paper_2509_26436_amd as q
-from test_decoding_refusals import EUNSUP, EWS, _attend
+from test_decoding_refusals import ESHAPE, EUNSUP, EWS, _append, _attend
 
 LONG = dict(width=4096, row=4096)     # a call that would go on to ask for its workspace
 
@@ -151,3 +151,9 @@ def test_append_into_its_own_inputs():
     assert append(whole, v, f=whole.view(-1).view(torch.int64)[:32]) == "share memory"
     # attention reads them only
     assert _answer(lambda: q.paged_attention(rows, q.PagedCache(whole, whole, table), pos)) == "on a GPU"
+
+
+def test_append_of_tables_past_32_bits():
+    for width in (-1, -(1 << 33), -(1 << 32) + 4, -(1 << 63), 1 << 31, 1 << 33):
+        for row in (4, 1 << 33):
+            assert _append(width=width, row=row) == ESHAPE, width
