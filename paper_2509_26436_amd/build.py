@@ -54,50 +54,53 @@ def binding_flags() -> tuple[list, list]:
     return compile_flags, link_flags
 
 
+def _compile(command: list, src: str, folder: str, verbose: bool) -> tuple:
+    """Compile one source of csrc into `folder`: (source, object, whether it failed, messages)."""
+    noise = "is not a recognized feature for this target"
+    obj = os.path.join(folder, os.path.splitext(src)[0] + ".o")
+    cmd = [*command, "-I", os.path.join(ROOT, "include"), "-I", CSRC, "-c", "-o", obj, os.path.join(CSRC, src)]
+    if verbose:
+        print(" ".join(cmd), flush=True)
+    res = subprocess.run(cmd, capture_output=True, text=True)
+    err = "\n".join(l for l in res.stderr.splitlines() if noise not in l)
+    return src, obj, res.returncode != 0, err
+
+
+def _objects(results: list, target: str, verbose: bool) -> list:
+    failed = [r[0] for r in results if r[2]]
+    for src, _, _, err in results:
+        if err.strip() and (verbose or failed):
+            sys.stderr.write(f"{src}:\n{err}\n")
+    if failed:
+        raise RuntimeError(f"compiling {os.path.basename(target)} failed: " + ", ".join(failed))
+    return [r[1] for r in results]
+
+
+def _link(target: str, command: list) -> None:
+    tmp = target + ".tmp"
+    res = subprocess.run([*command, "-o", tmp], capture_output=True, text=True)
+    if res.returncode != 0:
+        sys.stderr.write(res.stderr + "\n")
+        raise RuntimeError(f"linking {os.path.basename(target)} failed")
+    os.replace(tmp, target)
+
+
 def build(verbose: bool = False) -> str:
     """Compile every source to an object in parallel (each GEMM output mode is
-    its own translation unit), then link libquartz.so and the binding."""
+    its own translation unit), then link libquartz.so, which needs hipcc alone, and
+    after it the binding, which needs torch, Python's headers and g++ too."""
     import concurrent.futures
     import tempfile
 
-    noise = "is not a recognized feature for this target"
-    inc = ["-I", os.path.join(ROOT, "include"), "-I", CSRC]
     compile_flags = [f for f in HIPCC_FLAGS if f != "-shared"]
-    binding_compile, binding_link = binding_flags()
-    with tempfile.TemporaryDirectory(prefix="quartz_build_") as tmpdir:
-        def compile_one(src):
-            obj = os.path.join(tmpdir, os.path.splitext(src)[0] + ".o")
-            compiler = ["g++", *binding_compile] if src == BINDING_SOURCE else [hipcc(), *compile_flags]
-            cmd = [*compiler, *inc, "-c", "-o", obj, os.path.join(CSRC, src)]
-            if verbose:
-                print(" ".join(cmd), flush=True)
-            res = subprocess.run(cmd, capture_output=True, text=True)
-            err = "\n".join(l for l in res.stderr.splitlines() if noise not in l)
-            return src, obj, res.returncode, err
-
-        sources = [*SOURCES, BINDING_SOURCE]
-        workers = max(1, min(len(sources), os.cpu_count() or 1))
-        with concurrent.futures.ThreadPoolExecutor(max_workers=workers) as ex:
-            results = list(ex.map(compile_one, sources))
-        failed = [r for r in results if r[2] != 0]
-        for src, _, _, err in results:
-            if err.strip() and (verbose or failed):
-                sys.stderr.write(f"{src}:\n{err}\n")
-        if failed:
-            raise RuntimeError("compiling libquartz.so or its binding failed: " +
-                               ", ".join(r[0] for r in failed))
-        objects = {r[0]: r[1] for r in results}
-        binding = objects.pop(BINDING_SOURCE)
-
-        def link(target, cmd):
-            tmp = target + ".tmp"
-            res = subprocess.run([*cmd, "-o", tmp], capture_output=True, text=True)
-            if res.returncode != 0:
-                sys.stderr.write(res.stderr + "\n")
-                raise RuntimeError(f"linking {os.path.basename(target)} failed")
-            os.replace(tmp, target)
-        link(LIB, [hipcc(), "--offload-arch=gfx950", "-shared", "-fPIC", *objects.values()])
-        link(BINDING, ["g++", "-shared", "-fPIC", binding, *binding_link])
+    workers = max(1, min(len(SOURCES) + 1, os.cpu_count() or 1))
+    with tempfile.TemporaryDirectory(prefix="quartz_build_") as tmpdir, \
+            concurrent.futures.ThreadPoolExecutor(max_workers=workers) as ex:
+        binding = ex.submit(lambda: _compile(["g++", *binding_flags()[0]], BINDING_SOURCE, tmpdir, verbose))
+        results = list(ex.map(lambda src: _compile([hipcc(), *compile_flags], src, tmpdir, verbose), SOURCES))
+        _link(LIB, [hipcc(), "--offload-arch=gfx950", "-shared", "-fPIC", *_objects(results, LIB, verbose)])
+        _link(BINDING, ["g++", "-shared", "-fPIC", *_objects([binding.result()], BINDING, verbose),
+                        *binding_flags()[1]])
     return LIB
 
 
