@@ -67,9 +67,13 @@ __device__ __forceinline__ auto once(const uint8_t* p)
     return __builtin_nontemporal_load(reinterpret_cast<const words*>(p));
 }
 
-// 16 bytes of a key's row, whose 64-byte stretch an instruction reads.  Once is
-// better for 128 channels (8 heads of 262143 keys: 161 us, else 164) and worse
-// for 64 and 256 (32.1 against 29.5 us, 36.8 against 33.7).
+// 16 bytes of a key's row, whose 64-byte stretch an instruction reads.  Through the
+// caches but where blocks share heads of 128 channels.  Once, plain, caches in turn
+// (us): a block a head, 128 heads of 100 to 500 bf16 keys, 64 channels 8.2, 7.3, 128
+// channels 12.0, 10.2, 256 channels 21.0, 18.3; shared, 8 heads of 262143 bf16 keys,
+// 64 channels 95.1, 90.9; 128 channels, 512 heads of 129 to 4096 bf16 keys 99.6, 100.7,
+// e4m3 57.1, 59.1, 8 heads of 32768 e4m3 keys 20.3, 20.1; 256 channels, 128 heads of
+// 1000 to 16000 bf16 keys 188, 181.
 template <bool ONCE>
 __device__ __forceinline__ v4u load(const uint8_t* p)
 {
@@ -297,7 +301,7 @@ __global__ __launch_bounds__(64 * WAVES, SHARED ? fits(D, FP8) : 1) void paged_a
             for (int t = 0; t < 2; ++t)
 #pragma unroll
                 for (int s = 0; s < (FP8 ? kSteps / 2 : kSteps); ++s)
-                    kr[r][t][s] = load<D == 128>(p + 4 * t * D * kBytes + 64 * s);
+                    kr[r][t][s] = load<SHARED && D == 128>(p + 4 * t * D * kBytes + 64 * s);
         }
     };
     auto fetch_values = [&](int key0, const Pages& pages) {
@@ -641,9 +645,11 @@ int paged_blocks(int64_t sequences, int64_t heads, int64_t kv_heads, int64_t d, 
 {
     const int64_t parts = sequences * kv_heads * tiles_of(heads, kv_heads);
     // Few heads: a block a compute unit, whose long runs one after the other the
-    // memory serves best (8 heads of 262143 keys: 162 us, with three 173).  Many:
-    // as many as fit, so that one's change of heads is another's work (512 heads
-    // of 129 to 4096 e4m3 keys: 63 us with one, 54 with three).
+    // memory serves best.  Many: as many as fit, so that one's change of heads is
+    // another's work.  With one and three (us): 8 heads of 262144 bf16 keys 160, 169;
+    // 64 of 32768 168, 174, of 256 to 7782 30.5, 29.5; 128 of 16384 168, 174, of 1024
+    // to 31129 171, 172, as e4m3 95.8, 91.9; 512 of 256 to 7782 186, 174, as e4m3 118, 93
+    // (equal lengths of 4096 as e4m3: 89, 94).
     const int64_t compute_units = device_compute_units();
     const int64_t resident = compute_units * (4 * parts <= compute_units ? 1 : fits((int)d, fp8));
     // a window's first key may lie inside a tile
