@@ -164,10 +164,11 @@ __global__ __launch_bounds__(64 * kWaves) void mxfp4_dequantize_kernel(
     }
 }
 
-// Inputs past 128 MiB are no more in the last-level cache, with what else was
-// written since, and are read around it: 18432 x 4608 35.7 us so, 42.3 through it;
-// 4608 x 8192, still there, 17.4 and 16.6.
-constexpr int64_t kPastElements = (int64_t)1 << 26;
+// Inputs past 80 MiB are hardly in the last-level cache any more, with what else was
+// written since, and are read around it.  Around it and through it (us, three inputs
+// in turn): 4608 x 8192 (72 MiB) 18.1, 16.6; 6144 x 8192 (96) 23.1, 24.2; 8192 x 8192
+// 30.1, 31.2; 18432 x 4608 37.8, 39.7; 30000 x 8192 98, 112.
+constexpr int64_t kPastElements = (int64_t)5 << 23;
 
 // blocks of one launch; M K / 64 <= 2^28 keeps the items below 2^25
 uint32_t grid_of(int64_t M, uint32_t words)
