@@ -564,7 +564,7 @@ int64_t quartz_w4a4_linear_schedule(int64_t M, int64_t N, int64_t K, int32_t blo
  * quartz_mxfp4_dequantize: the values they stand for, y bf16 [M][ldy] (exact;
  *   beyond bf16's range infinite), ldy as ldx.
  * quartz_mxfp4_linear: y[m][n] = bf16(act(sum over k of a[m][k] w[n][k] + bias[n])),
- *   a and w the values of two MXFP4 tensors, products exact, sums in fp32.
+ *   a and w the values of two MXFP4 tensors, K > 0, products exact, sums in fp32.
  *   bias bf16 [N] or NULL; y bf16 [M][ldy], N <= ldy <= 2^24; epilogue
  *   QUARTZ_EPI_NONE or QUARTZ_EPI_GELU_TANH.  M = 0 or N = 0: nothing is done.
  * quartz_mxfp4_linear_bf16: the same from bf16 activations x [M][ldx], which are
@@ -616,7 +616,9 @@ quartz_status quartz_mxfp4_linear_kernel(int64_t M, int64_t N, int64_t K, int32_
  *   d, rot     even, 0 <= rot <= d.
  *   positions  int32 [tokens], any value.
  *   freqs      int64 [rot / 2]: f_i in units of 2^-64 turns, so that p f_i modulo
- *              one turn is the 64-bit product (exact for every position).
+ *              one turn is the 64-bit product (exact for every position).  Sine and
+ *              cosine are the device's, of the product's top bits: off by at most
+ *              3.2e-7 at any position.
  *
  * quartz_rotary_frequencies (host only, needs no GPU): freqs (HOST memory) of
  * f_i = base^(-2i / rot) / (2 pi), for longer contexts scaled by `factor` >= 1:
@@ -669,8 +671,9 @@ quartz_status quartz_rotary(const void* x_bf16, void* y_bf16, int64_t tokens, in
  * are clamped to [0, table_pages page_size]; positions without a page have no
  * weight, and what the cache holds in places that do not count (infinities and
  * NaN too) does not matter.  Without any key, or if every score is -inf, the output
- * is 0.  Scores and sums are fp32: scale k_scale log2(e) has to be 0 or a normal
- * fp32 number, and v_scale at least 2^-96 (QUARTZ_ERR_UNSUPPORTED otherwise).
+ * is 0.  Scores and sums are fp32, weights hold 16 bits: scale k_scale log2(e)
+ * has to be 0 or a normal fp32 number, and v_scale at least 2^-96
+ * (QUARTZ_ERR_UNSUPPORTED otherwise).
  *   q, o       bf16 [sequences][heads][d], strides in elements: multiples of 8
  *              for q, of 4 for o (whose pointer needs 8-byte alignment).
  *   table      row b belongs to sequence b (rows = sequences).

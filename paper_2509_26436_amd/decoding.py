@@ -4,8 +4,11 @@ and attention of one new token a sequence over a paged cache (include/quartz.h, 
 As in the rest of the package, the functions named like the C entry points take raw integers and
 return the status code; the tensor helpers check their tensors (``ValueError``), allocate outputs on
 the inputs' device (as memory of ``stream``, where one is given) and raise ``QuartzError`` on a
-non-OK status.  They launch on the inputs' device, whichever device is current.  The helpers'
-marshalling is compiled: a decoding step is many calls of a few microseconds.
+non-OK status.  They launch on the inputs' device, whichever device is current.  Outputs and
+workspaces that share memory with an input are a ``ValueError`` too.  Nothing is recorded for
+autograd: outputs require no gradient, whatever the inputs do (``rotary(inverse=True)`` is there for
+a caller's own backward pass).  The helpers' marshalling is compiled: a decoding step is many calls
+of a few microseconds.
 """
 from __future__ import annotations
 
@@ -234,7 +237,7 @@ def rotary(x, positions, freqs, layout: str = "half", inverse: bool = False, mag
     2 len(freqs) channels of every head turned by its token's position, the others copied.
     ``positions``: int32 [tokens].  ``layout`` pairs channels: "half" (i, i + len(freqs)) or
     "interleaved" (2i, 2i + 1).  ``inverse=True`` is the transposed map: it takes the gradient of
-    the output to that of the input.  ``out`` may be x."""
+    the output to that of the input (a caller's own backward pass calls it).  ``out`` may be x."""
     if stream is not None:
         with _On(stream, x):
             return rotary(x, positions, freqs, layout, inverse, magnitude, out)
@@ -257,7 +260,8 @@ def paged_append(cache: PagedCache, k, v, positions, sequences=None, freqs=None,
     """Writes the keys and values of new tokens, bf16 [tokens, heads, d] (any token and head
     strides), into the places of ``positions`` (int32 [tokens]) of ``sequences`` (int32 [tokens],
     rows of the table; None: token t is of sequence t).  ``freqs`` turns the keys on the way, as
-    ``rotary`` does.  Tokens without a place (negative positions, pages that are none) are skipped."""
+    ``rotary`` does.  Tokens without a place (negative positions, pages that are none) are skipped.
+    The cache's keys and values must be distinct memory, and none of the inputs'."""
     if stream is not None:
         with _On(stream, k):
             return paged_append(cache, k, v, positions, sequences, freqs, layout, magnitude)
@@ -280,7 +284,9 @@ def paged_attention(q, cache: PagedCache, lengths, scale: float | None = None, w
     """Attention of one new token a sequence over the first ``lengths`` (int32 [sequences], on the
     GPU) positions of its pages, or the last ``window`` of them: q bf16 [sequences, heads, d] ->
     bf16 [sequences, heads, d].  heads is a multiple of the cache's heads (neighbouring query heads
-    share one); ``scale`` is 1 / sqrt(d) by default.  A sequence of length 0 gives zeros."""
+    share one); ``scale`` is 1 / sqrt(d) by default.  A sequence of length 0 gives zeros.  The kernel
+    is chosen by the table's width (or the window): a table as wide as the longest sequence of a
+    few hundred keys takes one launch."""
     if stream is not None:
         with _On(stream, q):
             return paged_attention(q, cache, lengths, scale, window, out, workspace)
