@@ -358,6 +358,12 @@ PyObject* dequantize(PyObject*, PyObject* const* a, Py_ssize_t n)
     END_HANDLE_TH_ERRORS
 }
 
+// the columns of a layer's output that it writes
+Tensor written(const Tensor& out, int64_t N)
+{
+    return out.defined() && out.dim() == 2 && out.size(1) > N ? out.narrow(1, 0, N) : out;
+}
+
 // checks bias and out of a layer [M, N]; returns ldy
 int64_t layer_out(const Tensor& on, int64_t M, int64_t N, const Tensor& bias, Tensor& out)
 {
@@ -382,7 +388,7 @@ PyObject* linear_mx(PyObject*, PyObject* const* a, Py_ssize_t n)
     const int32_t epilogue = small(a[9], "epilogue");
     Tensor out = optional(a[10], "out");
     NEED(x.K == w.K, "K mismatch between activations and weights");
-    fresh(out, x.codes, x.scales, w.codes, w.scales, bias);
+    fresh(written(out, w.rows), x.codes, x.scales, w.codes, w.scales, bias);
     same_device(w.codes, x.codes, bias, out);
     const int64_t ldy = layer_out(w.codes, x.rows, w.rows, bias, out);
     launch("quartz_mxfp4_linear", out, [&](hipStream_t s) {
@@ -415,7 +421,7 @@ PyObject* linear_bf16(PyObject*, PyObject* const* a, Py_ssize_t n)
     Tensor out = optional(a[7], "out"), workspace = optional(a[8], "workspace");
     const int64_t ldx = rows_of(x, "x"), M = x.size(0);
     NEED(x.size(1) == w.K, "K mismatch between activations and weights");
-    fresh(out, x, w.codes, w.scales, bias, workspace);
+    fresh(written(out, w.rows), x, w.codes, w.scales, bias, workspace);
     scratch(workspace, x, w.codes, w.scales, bias);
     same_device(x, w.codes, bias, out, workspace);
     const int64_t ldy = layer_out(x, M, w.rows, bias, out);

@@ -157,3 +157,20 @@ def test_append_of_tables_past_32_bits():
     for width in (-1, -(1 << 33), -(1 << 32) + 4, -(1 << 63), 1 << 31, 1 << 33):
         for row in (4, 1 << 33):
             assert _append(width=width, row=row) == ESHAPE, width
+
+
+def test_columns_of_an_output_that_are_not_written():
+    """Of an output wider than the layer only the first N columns count: an input may lie in the others,
+    and rows may be closer than the view is wide."""
+    import torch
+    bf16 = torch.bfloat16
+    w = q.MxTensor(torch.zeros((2, 64, 16), dtype=torch.uint8), torch.zeros((1, 64, 4), dtype=torch.uint8), 64, 64)
+    rows = torch.zeros((8, 128), dtype=bf16)
+    t = q.MxTensor(torch.zeros((2, 8, 16), dtype=torch.uint8), torch.zeros((1, 8, 4), dtype=torch.uint8), 8, 64)
+    for call in (lambda out, x=rows[:, 64:]: q.mxfp4_linear(x, w, out=out), lambda out: q.mxfp4_linear(t, w, out=out)):
+        assert _answer(lambda: call(rows)) == "on a GPU"
+        assert _answer(lambda: call(rows.as_strided((8, 80), (128, 1)))) == "on a GPU"
+        assert _answer(lambda: call(torch.zeros(800, dtype=bf16).as_strided((8, 100), (64, 1)))) == "on a GPU"
+        assert _answer(lambda: call(torch.zeros(800, dtype=bf16).as_strided((8, 64), (63, 1)))) == "twice"
+    assert _answer(lambda: q.mxfp4_linear(rows[:, :64], w, out=rows)) == "share memory"
+    assert _answer(lambda: q.mxfp4_linear(rows[:, 56:120], w, out=rows)) == "share memory"
