@@ -655,25 +655,27 @@ int paged_blocks(int64_t sequences, int64_t heads, int64_t kv_heads, int64_t d, 
     // a window's first key may lie inside a tile
     const int64_t unit = unit_keys((int)d, fp8, true), units = (longest + kKeys - 1 + unit - 1) / unit;
     // A block a head (one launch) where that is at most 4 passes of its waves, or 8
-    // with a head for every compute unit.  32 heads of 512 e4m3 keys (2 passes):
-    // 7.1 us against 9.3 shared; of 1000 bf16 keys (8) 12.8 and 10.0; 512 heads of
-    // 100 to 1000 e4m3 keys (4) 21.2 and 22.5, of 1900 to 2000 (8) 45.9 and 49.5
-    // (of 100 to 2000, uneven, 36.4 and 32.3), of 100 to 2000 bf16 keys (16) 62.6
-    // and 51.4.
+    // with a head for every compute unit.  So, and shared (us, caches in turn): 32
+    // heads of 512 e4m3 keys (2 passes) 7.7, 9.5; of 1000 (4) 11.1, 10.0; of 1000 bf16
+    // keys (8) 14.7, 11.1; 256 heads of 1000 to 1024 bf16 keys (8) 26.7, 32.7; 512 heads
+    // of 1900 to 2000 e4m3 keys (8) 48.1, 56.8, of 100 to 2000 33.6, 36.1, of as many
+    // bf16 keys (16, where one long head may hold up a call) 55.8, 57.4.
     const int64_t pass = unit_keys((int)d, fp8, false), passes = (longest + pass - 1) / pass;
     if (passes <= 4 || (passes <= 8 && parts >= compute_units))
         return 0;
     return (int)std::min(resident, parts * units);
 }
 
-// Four, or where there are few keys as many as have some to read: 1976 heads of
-// up to 128 e4m3 keys 10.3 us with one, 12.7 with two, 17.0 with four; 32 heads of
-// 120 bf16 keys 5.7, 4.7 and 4.8.  (Eight, of 333 keys, take what four do.)
+// Four, or where there are few keys two, and one where more than two blocks a
+// compute unit hide each other's latency.  With one and two (us), heads of up to 128
+// keys: 32 of bf16 7.0, 5.9 (four: 5.8); 512 of 64 channels 6.4, 5.9, of 128 9.0, 8.3,
+// of 256 12.9, 12.5; 640 7.1, 6.9; 9.6, 8.9; 14.5, 19.0; 1976 of 128 e4m3 channels
+// 12.8, 15.7 (four: 21.7).  (Eight, of 333 keys, take what four do.)
 int paged_waves(int64_t sequences, int64_t heads, int64_t kv_heads, int64_t longest)
 {
     if (longest > 128)
         return 4;
-    return sequences * kv_heads * tiles_of(heads, kv_heads) > device_compute_units() ? 1 : 2;
+    return sequences * kv_heads * tiles_of(heads, kv_heads) > 2 * device_compute_units() ? 1 : 2;
 }
 
 size_t paged_attention_bytes(int64_t d, int blocks)

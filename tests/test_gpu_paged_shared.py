@@ -169,7 +169,7 @@ def test_every_query_finds_its_key(name):
 
 @pytest.mark.parametrize("window", [0, 1, 50])
 @pytest.mark.parametrize("longest", [128, 512])
-@pytest.mark.parametrize("kv,group,d,fp8", [(2, 4, 128, False), (3, 5, 128, True), (16, 2, 64, False),
+@pytest.mark.parametrize("kv,group,d,fp8", [(2, 4, 128, False), (3, 5, 128, True), (32, 2, 64, False),
                                             (2, 20, 64, True), (4, 1, 256, False), (1, 3, 256, True)])
 def test_a_block_a_head(kv, group, d, fp8, longest, window):
     """The same two in one launch: blocks of one (many heads), two and four waves; lengths around every
