@@ -710,6 +710,105 @@ quartz_status quartz_paged_attention(const void* q_bf16, void* o_bf16, int64_t s
                                      int64_t window, void* workspace, size_t workspace_bytes,
                                      hipStream_t stream);
 
+/*
+ * Prompts and drafted tokens over the paged cache.
+ *
+ * quartz_head_norm_rotary: the heads of queries and keys normed and turned,
+ *   y = R(w x / sqrt(mean x^2 + eps)),
+ * mean over a head's d channels, R as of quartz_rotary.  Positions may have several
+ * axes (time, height, width): pair i turns by the token's position on axis axes[i].
+ *   q, k       bf16 [tokens][q_heads (k_heads)][d], unit stride along d, the other
+ *              strides in elements (any); *_out likewise, in place with equal strides.
+ *              q_heads (k_heads) 0: none.  d even, up to 512.
+ *   *_weight   bf16 [d], NULL: ones.
+ *   positions  int32 [axis_count][axis_stride], tokens of each used.
+ *   axes       int32 [rot / 2], NULL: axis 0.  A pair of an axis that is none stays.
+ *   norm       0: no norm (weights NULL, eps not read).
+ * Sums, norms and rotations are fp32, rounded once.  Squares past fp32's range make
+ * a head zero.
+ *
+ * quartz_paged_prompt_attention: for the new tokens of each sequence
+ *   o[t][h] = sum_j p_j v_j,  p = softmax over j of b(scale q[t][h] . k_j).
+ *   starts     int32 [sequences + 1]: sequence b has the tokens starts[b] ..
+ *              starts[b + 1] - 1 (rows of q and o), at the last positions of its
+ *              lengths[b] (int32 [sequences]) keys, which hold them already.  Starts
+ *              are clamped to [0, tokens] and lengths to the table; rows of no
+ *              sequence are neither read nor written.
+ *   A token at position p sees the positions j <= p, the last `window` of them if
+ *   that is set, and those below prefix[b] (int32 [sequences], NULL: none) of its
+ *   sequence.
+ *   cap        0, or from 2^-10 to 1024: scores s become cap tanh(s / cap).
+ *   slopes     fp32 [heads], NULL: none; slopes[h] |p - j| is taken off a score
+ *              (after the cap).
+ * quartz_paged_tree_attention: the same for a tree of drafted tokens: a token sees
+ * every position before its sequence's new ones, and of those the ones that its bits
+ * name (bit i % 64 of tree[t][i / 64]: the sequence's new token i; its own bit
+ * counts too).  tree uint64 [tokens][tree_stride], tree_words used.
+ *
+ * Of both: q, o, scales, cache and table as for quartz_paged_attention, o zero where
+ * a token sees no key or only scores of -inf.  What the cache holds in places that a
+ * token does not see does not matter to it.  Weights hold 11 bits beside bf16 values
+ * that fp16 takes (0 or 2^-24 <= |v| < 2^9) or e4m3 ones, else 16; sums are fp32,
+ * of values times 2^14.  workspace: quartz_paged_prompt_workspace_bytes, as for
+ * quartz_paged_attention.  The host reads no starts or lengths: a call may be captured
+ * into a graph and replayed with others.
+ *
+ * quartz_paged_keep: the accepted tokens of a tree, moved to the places behind their
+ * sequence: position first[b] + kept[b][i] to first[b] + i for i < most, in keys and
+ * values.  first int32 [sequences], kept int32 [sequences][kept_stride]; entries
+ * below i (-1: none) move nothing, and nothing moves from or to a place without a
+ * page.  All positions are read as they were before the call.  Pages of two
+ * sequences must differ where they are written.
+ */
+quartz_status quartz_head_norm_rotary(const void* q_bf16, void* q_out_bf16, int64_t q_heads,
+                                      int64_t q_token, int64_t q_head, int64_t q_out_token,
+                                      int64_t q_out_head, const void* q_weight_bf16,
+                                      const void* k_bf16, void* k_out_bf16, int64_t k_heads,
+                                      int64_t k_token, int64_t k_head, int64_t k_out_token,
+                                      int64_t k_out_head, const void* k_weight_bf16, int64_t tokens,
+                                      int64_t d, int64_t rot, const int32_t* positions,
+                                      int64_t axis_count, int64_t axis_stride, const int32_t* axes,
+                                      const int64_t* freqs, int32_t layout, int32_t norm, float eps,
+                                      float magnitude, hipStream_t stream);
+
+size_t quartz_paged_prompt_workspace_bytes(int64_t tokens, int64_t sequences, int64_t heads,
+                                           int64_t kv_heads, int64_t d, int64_t page_size,
+                                           int64_t table_pages);
+
+quartz_status quartz_paged_prompt_attention(const void* q_bf16, void* o_bf16, int64_t tokens,
+                                            int64_t sequences, int64_t heads, int64_t kv_heads,
+                                            int64_t d, int64_t q_token, int64_t q_head,
+                                            int64_t o_token, int64_t o_head, const void* k_cache,
+                                            const void* v_cache, int32_t cache_type, float k_scale,
+                                            float v_scale, int64_t pages, int64_t page_size,
+                                            int64_t page_stride, const int32_t* table,
+                                            int64_t table_pages, int64_t table_stride,
+                                            const int32_t* starts, const int32_t* lengths,
+                                            float scale, int64_t window, float cap,
+                                            const float* slopes, const int32_t* prefix,
+                                            void* workspace, size_t workspace_bytes,
+                                            hipStream_t stream);
+
+quartz_status quartz_paged_tree_attention(const void* q_bf16, void* o_bf16, int64_t tokens,
+                                          int64_t sequences, int64_t heads, int64_t kv_heads,
+                                          int64_t d, int64_t q_token, int64_t q_head,
+                                          int64_t o_token, int64_t o_head, const void* k_cache,
+                                          const void* v_cache, int32_t cache_type, float k_scale,
+                                          float v_scale, int64_t pages, int64_t page_size,
+                                          int64_t page_stride, const int32_t* table,
+                                          int64_t table_pages, int64_t table_stride,
+                                          const int32_t* starts, const int32_t* lengths,
+                                          const uint64_t* tree, int64_t tree_words,
+                                          int64_t tree_stride, float scale, float cap,
+                                          void* workspace, size_t workspace_bytes,
+                                          hipStream_t stream);
+
+quartz_status quartz_paged_keep(const int32_t* first, const int32_t* kept, int64_t sequences,
+                                int64_t most, int64_t kept_stride, void* k_cache, void* v_cache,
+                                int32_t cache_type, int64_t heads, int64_t d, int64_t pages,
+                                int64_t page_size, int64_t page_stride, const int32_t* table,
+                                int64_t table_pages, int64_t table_stride, hipStream_t stream);
+
 /* Static, NUL-terminated description of a status code (host memory). */
 const char* quartz_status_string(quartz_status s);
 

@@ -38,9 +38,12 @@ __all__ = [
     "quartz_mxfp4_linear_workspace_bytes", "quartz_mxfp4_linear_bf16", "quartz_mxfp4_linear_kernel",
     "quartz_rotary_frequencies", "quartz_rotary", "quartz_paged_append",
     "quartz_paged_attention_workspace_bytes", "quartz_paged_attention",
+    "quartz_head_norm_rotary", "quartz_paged_prompt_workspace_bytes", "quartz_paged_prompt_attention",
+    "quartz_paged_tree_attention", "quartz_paged_keep",
     "MxTensor", "PagedCache", "mxfp4_quantize", "mxfp4_dequantize", "mxfp4_linear",
     "mxfp4_workspace", "mxfp4_linear_kernel", "rotary_frequencies", "rotary", "paged_append", "paged_attention",
-    "paged_attention_workspace",
+    "paged_attention_workspace", "head_norm_rotary", "paged_prompt_attention", "paged_prompt_workspace",
+    "paged_tree_attention", "paged_keep",
 ]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -70,6 +73,8 @@ EXPORTED_SYMBOLS = (
     "quartz_mxfp4_linear_workspace_bytes", "quartz_mxfp4_linear_bf16", "quartz_mxfp4_linear_kernel",
     "quartz_rotary_frequencies", "quartz_rotary", "quartz_paged_append",
     "quartz_paged_attention_workspace_bytes", "quartz_paged_attention",
+    "quartz_head_norm_rotary", "quartz_paged_prompt_workspace_bytes", "quartz_paged_prompt_attention",
+    "quartz_paged_tree_attention", "quartz_paged_keep",
 )
 
 
@@ -818,10 +823,12 @@ def lzs_attention(q, k, v, heads: int, lzs_group: int = 16, out=None, workspace=
 
 
 from .decoding import (  # noqa: E402  (it uses the definitions above)
-    MxTensor, PagedCache, mxfp4_dequantize, mxfp4_linear, mxfp4_linear_kernel, mxfp4_quantize,
-    mxfp4_workspace, paged_append, paged_attention, paged_attention_workspace,
+    MxTensor, PagedCache, head_norm_rotary, mxfp4_dequantize, mxfp4_linear, mxfp4_linear_kernel,
+    mxfp4_quantize, mxfp4_workspace, paged_append, paged_attention, paged_attention_workspace, paged_keep,
+    paged_prompt_attention, paged_prompt_workspace, paged_tree_attention, quartz_head_norm_rotary,
     quartz_mxfp4_dequantize, quartz_mxfp4_linear, quartz_mxfp4_linear_bf16,
     quartz_mxfp4_linear_kernel, quartz_mxfp4_linear_workspace_bytes,
     quartz_mxfp4_quantize, quartz_paged_append, quartz_paged_attention,
-    quartz_paged_attention_workspace_bytes, quartz_rotary, quartz_rotary_frequencies, rotary,
-    rotary_frequencies)
+    quartz_paged_attention_workspace_bytes, quartz_paged_keep, quartz_paged_prompt_attention,
+    quartz_paged_prompt_workspace_bytes, quartz_paged_tree_attention, quartz_rotary,
+    quartz_rotary_frequencies, rotary, rotary_frequencies)

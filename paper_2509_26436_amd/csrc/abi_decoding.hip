@@ -24,6 +24,12 @@ constexpr int64_t kMaxPositions = int64_t(1) << 30;
 constexpr int64_t kMaxStride = int64_t(1) << 40;
 // attention's v_scale: over a sum of weights of up to kMaxPositions still normal
 constexpr float kMinValueScale = 0x1p-96f;
+// channels of a normed head: 64 lanes of four pairs
+constexpr int64_t kMaxNorm = 512;
+// query rows of one call of several tokens a sequence
+constexpr int64_t kMaxRows = int64_t(1) << 30;
+// caps of scores: the tanh is off by 2e-7, times the cap
+constexpr float kMinCap = 0x1p-10f, kMaxCap = 1024.0f;
 
 bool layout_ok(int32_t layout) { return layout == QUARTZ_ROTARY_HALF || layout == QUARTZ_ROTARY_INTERLEAVED; }
 
@@ -385,6 +391,220 @@ quartz_status quartz_paged_attention(const void* q_bf16, void* o_bf16, int64_t s
     a.waves = paged_waves(sequences, heads, kv_heads, longest);
     a.workspace = static_cast<float*>(workspace);
     return from_hip(launch_paged_attention(a, stream));
+}
+
+quartz_status quartz_head_norm_rotary(const void* q_bf16, void* q_out, int64_t q_heads, int64_t q_token, int64_t q_head,
+                                      int64_t q_out_token, int64_t q_out_head, const void* q_weight,
+                                      const void* k_bf16, void* k_out, int64_t k_heads, int64_t k_token,
+                                      int64_t k_head, int64_t k_out_token, int64_t k_out_head, const void* k_weight,
+                                      int64_t tokens, int64_t d, int64_t rot, const int32_t* positions,
+                                      int64_t axis_count, int64_t axis_stride, const int32_t* axes,
+                                      const int64_t* freqs, int32_t layout, int32_t norm, float eps, float magnitude,
+                                      hipStream_t stream)
+{
+    if (!layout_ok(layout) || !std::isfinite(magnitude) || (norm != 0 && (!(eps >= 0.0f) || !std::isfinite(eps))) ||
+        (norm == 0 && (q_weight || k_weight)))
+        return QUARTZ_ERR_UNSUPPORTED;
+    if (tokens < 0 || q_heads < 0 || q_heads > kMaxK || k_heads < 0 || k_heads > kMaxK || d <= 0 || d > kMaxNorm ||
+        d % 2 != 0 || rot < 0 || rot > d || rot % 2 != 0 || axis_count < 1 || axis_count > kMaxK ||
+        tokens > kMaxAppend || !product_ok((q_heads + k_heads) * d, tokens, kMaxAppend) || !stride_ok(axis_stride))
+        return QUARTZ_ERR_SHAPE;
+    for (const int64_t stride : {q_token, q_head, q_out_token, q_out_head, k_token, k_head, k_out_token, k_out_head})
+        if (!stride_ok(stride))
+            return QUARTZ_ERR_SHAPE;
+    HeadNorm a{};
+    a.q = {static_cast<const uint16_t*>(q_bf16), static_cast<uint16_t*>(q_out), static_cast<const uint16_t*>(q_weight),
+           (int32_t)q_heads, q_token, q_head, q_out_token, q_out_head};
+    a.k = {static_cast<const uint16_t*>(k_bf16), static_cast<uint16_t*>(k_out), static_cast<const uint16_t*>(k_weight),
+           (int32_t)k_heads, k_token, k_head, k_out_token, k_out_head};
+    if (tokens == 0 || q_heads + k_heads == 0)
+        return QUARTZ_OK;
+    if (rot > 0 && (!positions || !freqs))
+        return QUARTZ_ERR_NULL;
+    if (!aligned(positions, 4) || !aligned(axes, 4) || !aligned(freqs, 8))
+        return QUARTZ_ERR_ALIGN;
+    for (const HeadRows* r : {&a.q, &a.k}) {
+        if (r->heads == 0)
+            continue;
+        if (!r->x || !r->y)
+            return QUARTZ_ERR_NULL;
+        if (!aligned(r->x, 2) || !aligned(r->y, 2) || !aligned(r->weight, 2))
+            return QUARTZ_ERR_ALIGN;
+        if (r->x == r->y && (r->x_token != r->y_token || r->x_head != r->y_head))
+            return QUARTZ_ERR_SHAPE;   // in place: the same elements
+    }
+    a.tokens = tokens;
+    a.d = (int32_t)d;
+    a.rot = (int32_t)rot;
+    a.positions = positions;
+    a.axis_count = (int32_t)axis_count;
+    a.axis_stride = axis_stride;
+    a.axes = axes;
+    a.freqs = freqs;
+    a.interleaved = layout == QUARTZ_ROTARY_INTERLEAVED;
+    a.norm = norm != 0;
+    a.eps = eps;
+    a.magnitude = magnitude;
+    a.inverse_d = 1.0f / (float)d;
+    return from_hip(launch_head_norm(a, stream));
+}
+
+quartz_status quartz_paged_keep(const int32_t* first, const int32_t* kept, int64_t sequences, int64_t most,
+                                int64_t kept_stride, void* k_cache, void* v_cache, int32_t cache_type, int64_t heads,
+                                int64_t d, int64_t pages, int64_t page_size, int64_t page_stride,
+                                const int32_t* table, int64_t table_pages, int64_t table_stride, hipStream_t stream)
+{
+    if (sequences < 0 || most < 0 || most > kMaxPositions || heads <= 0 || heads > kMaxK ||
+        kept_stride < most || kept_stride > kMaxStride || !product_ok(sequences, heads, kMaxBlocks512) ||
+        d <= 0 || d > kMaxK || table_pages < 0 || table_pages > kMaxPositions)
+        return QUARTZ_ERR_SHAPE;
+    PagedKeep a{};
+    a.cache = {k_cache, v_cache, pages, page_stride, (int32_t)heads, (int32_t)d, shift_of(page_size),
+               cache_type == QUARTZ_CACHE_E4M3, 1.0f, 1.0f, table, sequences, table_stride, (int32_t)table_pages};
+    const bool used = sequences > 0 && most > 0;
+    const quartz_status st = cache_checks(a.cache, page_size, cache_type, used);
+    if (st != QUARTZ_OK || !used)
+        return st;
+    if (!first || !kept)
+        return QUARTZ_ERR_NULL;
+    if (!aligned(first, 4) || !aligned(kept, 4))
+        return QUARTZ_ERR_ALIGN;
+    if (table_pages == 0)
+        return QUARTZ_OK;              // nothing has a place
+    a.first = first;
+    a.kept = kept;
+    a.kept_stride = kept_stride;
+    a.most = most;
+    return from_hip(launch_paged_keep(a, stream));
+}
+
+// sizes of a call for several new tokens a sequence
+static quartz_status prompt_checks(int64_t tokens, int64_t sequences, int64_t heads, int64_t kv_heads, int64_t d,
+                                   int64_t page_size, int64_t table_pages)
+{
+    int64_t longest = 0;
+    const quartz_status st = attention_checks(sequences, heads, kv_heads, d, page_size, table_pages, 0, longest);
+    if (st != QUARTZ_OK)
+        return st;
+    return tokens < 0 || tokens > kMaxRows || !product_ok(tokens, heads, kMaxRows) ? QUARTZ_ERR_SHAPE : QUARTZ_OK;
+}
+
+size_t quartz_paged_prompt_workspace_bytes(int64_t tokens, int64_t sequences, int64_t heads, int64_t kv_heads,
+                                           int64_t d, int64_t page_size, int64_t table_pages)
+{
+    if (prompt_checks(tokens, sequences, heads, kv_heads, d, page_size, table_pages) != QUARTZ_OK || tokens == 0 ||
+        sequences == 0)
+        return 0;
+    return prompt_attention_bytes(prompt_shape(tokens, sequences, heads, kv_heads, d, table_pages * page_size), kv_heads, d);
+}
+
+// what the entry points of prompts and trees share; `a` has what only one of them takes
+static quartz_status prompt_attention(PromptAttention a, const void* q_bf16, void* o_bf16, int64_t tokens, int64_t sequences,
+                                      int64_t heads, int64_t kv_heads, int64_t d, int64_t q_token, int64_t q_head,
+                                      int64_t o_token, int64_t o_head, void* k_cache, void* v_cache,
+                                      int32_t cache_type, float k_scale, float v_scale, int64_t pages,
+                                      int64_t page_size, int64_t page_stride, const int32_t* table,
+                                      int64_t table_pages, int64_t table_stride, const int32_t* starts,
+                                      const int32_t* lengths, float scale, float cap, void* workspace,
+                                      size_t workspace_bytes, hipStream_t stream)
+{
+    // one factor for the scores, which fp32 has to hold with all its bits; capped: to 2 y log2(e) of tanh(y)
+    const double log2e = 1.4426950408889634;
+    if (!std::isfinite(scale) || !(cap >= 0.0f) || cap > kMaxCap || (cap > 0.0f && cap < kMinCap))
+        return QUARTZ_ERR_UNSUPPORTED;
+    const double factor = std::fabs((double)scale) * (double)k_scale * log2e * (cap > 0.0f ? 2.0 / cap : 1.0);
+    if ((factor != 0.0 && !std::isnormal((float)factor)) || v_scale < kMinValueScale)
+        return QUARTZ_ERR_UNSUPPORTED;
+    quartz_status st = prompt_checks(tokens, sequences, heads, kv_heads, d, page_size, table_pages);
+    if (st != QUARTZ_OK)
+        return st;
+    if (!stride_ok(q_token) || !stride_ok(q_head) || !stride_ok(o_token) || !stride_ok(o_head))
+        return QUARTZ_ERR_SHAPE;
+    a.cache = {k_cache, v_cache, pages, page_stride, (int32_t)kv_heads, (int32_t)d, shift_of(page_size),
+               cache_type == QUARTZ_CACHE_E4M3, k_scale, v_scale, table, sequences, table_stride,
+               (int32_t)table_pages};
+    const bool used = sequences > 0 && tokens > 0;
+    st = cache_checks(a.cache, page_size, cache_type, used);
+    if (st != QUARTZ_OK || !used)
+        return st;
+    if (!q_bf16 || !o_bf16 || !starts || !lengths)
+        return QUARTZ_ERR_NULL;
+    if (!aligned16(q_bf16) || !aligned(o_bf16, 8) || !aligned(starts, 4) || !aligned(lengths, 4) ||
+        !aligned16(workspace) || ((q_token | q_head) & 7) != 0 || ((o_token | o_head) & 3) != 0)
+        return QUARTZ_ERR_ALIGN;
+    const PromptShape s = prompt_shape(tokens, sequences, heads, kv_heads, d, table_pages * page_size);
+    const size_t need = prompt_attention_bytes(s, kv_heads, d);
+    if (need > 0 && (!workspace || workspace_bytes < need))
+        return QUARTZ_ERR_WORKSPACE;
+    a.q = static_cast<const uint16_t*>(q_bf16);
+    a.o = static_cast<uint16_t*>(o_bf16);
+    a.q_token = q_token;
+    a.q_head = q_head;
+    a.o_token = o_token;
+    a.o_head = o_head;
+    a.tokens = tokens;
+    a.heads = (int32_t)heads;
+    a.starts = starts;
+    a.lengths = lengths;
+    a.negate = scale < 0.0f;
+    a.scale = (float)factor;
+    a.cap = (float)(cap * log2e);
+    a.rows = s.rows;
+    a.splits = s.splits;
+    a.unit = s.unit;
+    a.tiles = s.tiles;
+    a.workspace = static_cast<float*>(workspace);
+    return from_hip(launch_prompt_attention(a, stream));
+}
+
+quartz_status quartz_paged_prompt_attention(const void* q_bf16, void* o_bf16, int64_t tokens, int64_t sequences,
+                                            int64_t heads, int64_t kv_heads, int64_t d, int64_t q_token,
+                                            int64_t q_head, int64_t o_token, int64_t o_head, const void* k_cache,
+                                            const void* v_cache, int32_t cache_type, float k_scale, float v_scale,
+                                            int64_t pages, int64_t page_size, int64_t page_stride,
+                                            const int32_t* table, int64_t table_pages, int64_t table_stride,
+                                            const int32_t* starts, const int32_t* lengths, float scale,
+                                            int64_t window, float cap, const float* slopes, const int32_t* prefix,
+                                            void* workspace, size_t workspace_bytes, hipStream_t stream)
+{
+    if (window < 0)
+        return QUARTZ_ERR_SHAPE;
+    if (!aligned(slopes, 4) || !aligned(prefix, 4))
+        return QUARTZ_ERR_ALIGN;
+    PromptAttention a{};
+    a.window = (int32_t)(window < kMaxPositions ? window : kMaxPositions);
+    a.slopes = slopes;
+    a.prefix = prefix;
+    return prompt_attention(a, q_bf16, o_bf16, tokens, sequences, heads, kv_heads, d, q_token, q_head, o_token, o_head,
+                            const_cast<void*>(k_cache), const_cast<void*>(v_cache), cache_type, k_scale, v_scale,
+                            pages, page_size, page_stride, table, table_pages, table_stride, starts, lengths, scale, cap,
+                            workspace, workspace_bytes, stream);
+}
+
+quartz_status quartz_paged_tree_attention(const void* q_bf16, void* o_bf16, int64_t tokens, int64_t sequences,
+                                          int64_t heads, int64_t kv_heads, int64_t d, int64_t q_token, int64_t q_head,
+                                          int64_t o_token, int64_t o_head, const void* k_cache, const void* v_cache,
+                                          int32_t cache_type, float k_scale, float v_scale, int64_t pages,
+                                          int64_t page_size, int64_t page_stride, const int32_t* table,
+                                          int64_t table_pages, int64_t table_stride, const int32_t* starts,
+                                          const int32_t* lengths, const uint64_t* tree, int64_t tree_words,
+                                          int64_t tree_stride, float scale, float cap, void* workspace,
+                                          size_t workspace_bytes, hipStream_t stream)
+{
+    if (tree_words < 1 || tree_words > kMaxK || !stride_ok(tree_stride))
+        return QUARTZ_ERR_SHAPE;
+    if (!tree && tokens > 0 && sequences > 0)
+        return QUARTZ_ERR_NULL;
+    if (!aligned(tree, 8))
+        return QUARTZ_ERR_ALIGN;
+    PromptAttention a{};
+    a.tree = tree;
+    a.tree_token = tree_stride;
+    a.tree_words = (int32_t)tree_words;
+    return prompt_attention(a, q_bf16, o_bf16, tokens, sequences, heads, kv_heads, d, q_token, q_head, o_token, o_head,
+                            const_cast<void*>(k_cache), const_cast<void*>(v_cache), cache_type, k_scale, v_scale,
+                            pages, page_size, page_stride, table, table_pages, table_stride, starts, lengths, scale, cap,
+                            workspace, workspace_bytes, stream);
 }
 
 }  // extern "C"

@@ -606,6 +606,146 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n)
     END_HANDLE_TH_ERRORS
 }
 
+// (q, k, positions, freqs, q_weight, k_weight, eps, axes, layout, magnitude, q_out, k_out) -> q_out, k_out
+PyObject* head_norm_rotary(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    ARGUMENTS(12)
+    const Tensor& q = tensor(a[0], "q");
+    const Tensor k = optional(a[1], "k"), &positions = tensor(a[2], "positions"), &freqs = tensor(a[3], "freqs");
+    const Tensor weight[2] = {optional(a[4], "q_weight"), optional(a[5], "k_weight")}, axes = optional(a[7], "axes");
+    heads_of(q, "q");
+    const int64_t tokens = q.size(0), d = q.size(2), rot = rotated(freqs, d);
+    if (k.defined()) {
+        heads_of(k, "k");
+        NEED(k.size(0) == tokens && k.size(2) == d, "k must be [tokens, heads, d] with q's tokens and d");
+    }
+    NEED(positions.scalar_type() == at::kInt && (positions.dim() == 1 || positions.dim() == 2) &&
+             positions.size(-1) == tokens && unit(positions, -1),
+         "positions must be int32 [tokens] or [axes, tokens] with unit stride along the tokens");
+    const int64_t axis_count = positions.dim() == 2 ? positions.size(0) : 1;
+    const int64_t axis_stride = positions.dim() == 2 ? stride_of(positions, 0) : 0;
+    NEED(axis_count > 0, "positions must have an axis");
+    const int32_t* axis = axes.defined() ? int32_of(axes, rot / 2, "axes") : nullptr;
+    const bool norm = a[6] != Py_None;
+    const float eps = norm ? (float)real(a[6]) : 0.0f, magnitude = (float)real(a[9]);
+    for (const Tensor& w : weight)
+        NEED(!w.defined() || (w.scalar_type() == at::kBFloat16 && w.dim() == 1 && w.size(0) == d && unit(w, 0)),
+             "weights must be bf16 [d], contiguous");
+    NEED(norm || (!weight[0].defined() && !weight[1].defined()), "weights belong to a norm (eps is None)");
+    NEED(k.defined() || !weight[1].defined(), "k_weight without k");
+    const int32_t layout = layout_of(a[8]);
+    const Tensor* x[2] = {&q, &k};
+    Tensor out[2] = {optional(a[10], "q_out"), optional(a[11], "k_out")};
+    NEED(k.defined() || !out[1].defined(), "k_out without k");
+    for (int i = 0; i < 2; ++i)
+        fresh(out[i], in_place(out[i], *x[i]) ? Tensor() : *x[i], *x[1 - i], positions, freqs, weight[0], weight[1], axes);
+    NEED(!share(out[0], out[1]), "the outputs must not share memory");
+    same_device(q, k, positions, freqs, weight[0], weight[1], axes, out[0], out[1]);
+    for (int i = 0; i < 2; ++i) {
+        if (!x[i]->defined())
+            continue;
+        if (!out[i].defined())
+            out[i] = at::empty(x[i]->sizes(), x[i]->options().requires_grad(false));
+        heads_of(out[i], "out");
+        NEED(out[i].sizes() == x[i]->sizes(), "outputs must have the inputs' shapes");
+    }
+    const auto stride = [](const Tensor& t, int64_t dim) { return t.defined() ? stride_of(t, dim) : 0; };
+    launch("quartz_head_norm_rotary", q, [&](hipStream_t s) {
+        return quartz_head_norm_rotary(
+            q.data_ptr(), out[0].data_ptr(), q.size(1), stride(q, 0), stride(q, 1), stride(out[0], 0), stride(out[0], 1),
+            address(weight[0]), address(k), address(out[1]), k.defined() ? k.size(1) : 0, stride(k, 0), stride(k, 1),
+            stride(out[1], 0), stride(out[1], 1), address(weight[1]), tokens, d, rot,
+            static_cast<const int32_t*>(positions.data_ptr()), axis_count, axis_stride, axis,
+            static_cast<const int64_t*>(freqs.data_ptr()), layout, norm, eps, magnitude, s);
+    });
+    PyObject* both = PyTuple_New(2);
+    for (int i = 0; i < 2; ++i) {
+        if (!x[i]->defined())
+            Py_INCREF(Py_None);
+        PyTuple_SET_ITEM(both, i, x[i]->defined() ? THPVariable_Wrap(std::move(out[i])) : Py_None);
+    }
+    return both;
+    END_HANDLE_TH_ERRORS
+}
+
+// (the cache's five, q, starts, lengths, tree, scale, window, cap, slopes, prefix, out, workspace) -> out
+PyObject* prompt_attention(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    ARGUMENTS(16)
+    const Cache c = cache_of(a[0], a[1], a[2], a[3], a[4]);
+    const Tensor &q = tensor(a[5], "q"), &starts = tensor(a[6], "starts"), &lengths = tensor(a[7], "lengths");
+    const Tensor tree = optional(a[8], "tree"), slopes = optional(a[12], "slopes"), prefix = optional(a[13], "prefix");
+    heads_of(q, "q");
+    const int64_t tokens = q.size(0), heads = q.size(1), d = q.size(2), sequences = c.table.size(0), window = integer(a[10]);
+    NEED(d == c.d && c.heads > 0 && heads % c.heads == 0,
+         "q must be [tokens, heads, d] with the cache's d and heads a multiple of the cache's");
+    const int32_t* first = int32_of(starts, sequences + 1, "starts");
+    const int32_t* len = int32_of(lengths, sequences, "lengths");
+    const int32_t* before = prefix.defined() ? int32_of(prefix, sequences, "prefix") : nullptr;
+    NEED(!slopes.defined() || (slopes.scalar_type() == at::kFloat && slopes.dim() == 1 && slopes.size(0) == heads && unit(slopes, 0)),
+         "slopes must be a contiguous fp32 tensor of ", heads);
+    NEED(!tree.defined() || (tree.scalar_type() == at::kLong && tree.dim() == 2 && tree.size(0) == tokens && tree.size(1) > 0 && unit(tree, 1)),
+         "tree must be an int64 [tokens, words] tensor with unit column stride");
+    const float scale = a[9] == Py_None ? (float)(1.0 / std::sqrt((double)d)) : (float)real(a[9]);
+    const float cap = (float)real(a[11]);
+    Tensor out = optional(a[14], "out"), workspace = optional(a[15], "workspace");
+    fresh(out, q, c.k, c.v, c.table, starts, lengths, tree, slopes, prefix, workspace);
+    scratch(workspace, q, c.k, c.v, c.table, starts, lengths, tree, slopes, prefix);
+    same_device(c.k, q, starts, lengths, tree, slopes, prefix, out, workspace);
+    const c10::hip::OptionalHIPGuard guard(q.device().index());    // the workspace is sized for its compute units
+    if (!out.defined())
+        out = at::empty({tokens, heads, d}, q.options().requires_grad(false));
+    heads_of(out, "out");
+    NEED(out.sizes() == q.sizes(), "out must have q's shape");
+    const size_t size = workspace_of(
+        workspace, quartz_paged_prompt_workspace_bytes(tokens, sequences, heads, c.heads, d, c.page, c.table.size(1)), q);
+    const auto call = [&](auto entry, auto... own) {
+        return [&, entry, own...](hipStream_t s) {
+            return entry(q.data_ptr(), out.data_ptr(), tokens, sequences, heads, c.heads, d, stride_of(q, 0),
+                         stride_of(q, 1), stride_of(out, 0), stride_of(out, 1), c.k.data_ptr(), c.v.data_ptr(), c.type,
+                         c.k_scale, c.v_scale, c.pages, c.page, c.stride, table_at(c), c.table.size(1), table_stride(c),
+                         first, len, own..., address(workspace), size, s);
+        };
+    };
+    if (tree.defined())
+        launch("quartz_paged_tree_attention", q,
+               call(quartz_paged_tree_attention, static_cast<const uint64_t*>(tree.data_ptr()), tree.size(1),
+                    stride_of(tree, 0), scale, cap));
+    else
+        launch("quartz_paged_prompt_attention", q,
+               call(quartz_paged_prompt_attention, scale, window, cap, static_cast<const float*>(address(slopes)), before));
+    return THPVariable_Wrap(std::move(out));
+    END_HANDLE_TH_ERRORS
+}
+
+// (the cache's five, first, kept)
+PyObject* keep(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    ARGUMENTS(7)
+    const Cache c = cache_of(a[0], a[1], a[2], a[3], a[4]);
+    const Tensor &first = tensor(a[5], "first"), &kept = tensor(a[6], "kept");
+    const int64_t sequences = c.table.size(0);
+    const int32_t* begin = int32_of(first, sequences, "first");
+    NEED(kept.scalar_type() == at::kInt && kept.dim() == 2 && kept.size(0) == sequences && unit(kept, 1),
+         "kept must be an int32 [sequences, most] tensor with unit column stride, a row of the table a sequence");
+    NEED(!strided(kept, 0) || kept.stride(0) >= kept.size(1), "the rows of kept must not overlap");
+    NEED(!share(c.k, c.v), "the cache's keys and values must not share memory");
+    for (const Tensor* pages : {&c.k, &c.v})
+        NEED(!share(*pages, first) && !share(*pages, kept) && !share(*pages, c.table),
+             "the cache must not share memory with an input");
+    same_device(c.k, first, kept);
+    launch("quartz_paged_keep", c.k, [&](hipStream_t s) {
+        return quartz_paged_keep(begin, static_cast<const int32_t*>(kept.data_ptr()), sequences, kept.size(1),
+                                 strided(kept, 0) ? kept.stride(0) : kept.size(1), c.k.data_ptr(), c.v.data_ptr(), c.type,
+                                 c.heads, c.d, c.pages, c.page, c.stride, table_at(c), c.table.size(1), table_stride(c), s);
+    });
+    Py_RETURN_NONE;
+    END_HANDLE_TH_ERRORS
+}
+
 template <PyObject* (*F)(PyObject*, PyObject* const*, Py_ssize_t)>
 PyCFunction fast() { return reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(F)); }
 
@@ -620,6 +760,9 @@ PyMethodDef kMethods[] = {
     {"check_cache", fast<check_cache>(), METH_FASTCALL, nullptr},
     {"append", fast<append>(), METH_FASTCALL, nullptr},
     {"attention", fast<attention>(), METH_FASTCALL, nullptr},
+    {"head_norm_rotary", fast<head_norm_rotary>(), METH_FASTCALL, nullptr},
+    {"prompt_attention", fast<prompt_attention>(), METH_FASTCALL, nullptr},
+    {"keep", fast<keep>(), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 

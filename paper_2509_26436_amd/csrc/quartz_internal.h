@@ -307,6 +307,28 @@ struct Rotary {
 };
 hipError_t launch_rotary(const Rotary& a, hipStream_t stream);
 
+// Norms of query and key heads, turned: rows of either (heads 0: none).
+struct HeadRows {
+    const uint16_t* x;
+    uint16_t* y;              // may be x, with the same strides
+    const uint16_t* weight;   // nullptr: ones
+    int32_t heads;
+    int64_t x_token, x_head, y_token, y_head;
+};
+struct HeadNorm {
+    HeadRows q, k;
+    int64_t tokens;
+    int32_t d, rot;
+    const int32_t* positions; // of an axis, axis_stride apart
+    int64_t axis_stride;
+    int32_t axis_count;
+    const int32_t* axes;      // of each pair; nullptr: 0
+    const int64_t* freqs;
+    bool interleaved, norm;
+    float magnitude, eps, inverse_d;
+};
+hipError_t launch_head_norm(const HeadNorm& a, hipStream_t stream);
+
 // A layer's paged cache: k and v [pages][heads][page][d] of bf16 or e4m3
 // (page_stride elements from a page to the next), a stored value standing for
 // itself times the scale; row s of the table [sequences][table_stride] holds
@@ -337,6 +359,15 @@ struct PagedAppend {
 };
 hipError_t launch_paged_append(const PagedAppend& a, hipStream_t stream);
 
+// Places first[b] + kept[b][i] of sequence b to first[b] + i, for kept[b][i] > i.
+struct PagedKeep {
+    PagedCacheView cache;
+    const int32_t* first;
+    const int32_t* kept;
+    int64_t kept_stride, most;
+};
+hipError_t launch_paged_keep(const PagedKeep& a, hipStream_t stream);
+
 // One new token a sequence: o [sequences][heads][d] from q.
 struct PagedAttention {
     PagedCacheView cache;     // .sequences: the batch
@@ -358,6 +389,40 @@ int paged_blocks(int64_t sequences, int64_t heads, int64_t kv_heads, int64_t d, 
 int paged_waves(int64_t sequences, int64_t heads, int64_t kv_heads, int64_t longest);
 size_t paged_attention_bytes(int64_t d, int blocks);
 hipError_t launch_paged_attention(const PagedAttention& a, hipStream_t stream);
+
+// Several new tokens a sequence: tokens starts[b] .. starts[b + 1] - 1 of sequence
+// b, at the last places of its lengths[b] keys.
+struct PromptShape {
+    int32_t rows;             // of a block's tile: 32, 64, 128 or 256
+    int32_t splits;           // parts that a tile's keys are cut into at most
+    int32_t unit;             // keys of a part at least
+    int64_t tiles;            // of any division of the tokens at most
+};
+struct PromptAttention {
+    PagedCacheView cache;     // .sequences: the batch
+    const uint16_t* q;
+    uint16_t* o;
+    int64_t q_token, q_head, o_token, o_head;
+    int64_t tokens;
+    int32_t heads;            // of q: a multiple of cache.heads
+    const int32_t* starts;
+    const int32_t* lengths;
+    const int32_t* prefix;    // nullptr: none
+    const float* slopes;      // nullptr: none
+    const uint64_t* tree;     // nullptr: causal; else tree_words words a token
+    int64_t tree_token;
+    int32_t tree_words;
+    bool negate;              // the sign of the scale
+    float scale;              // of q . k to scores in units of log2 (capped: to the exponent of their tanh)
+    float cap;                // in units of log2; 0: none
+    int32_t window;           // 0: all keys
+    int32_t rows, splits, unit;
+    int64_t tiles;            // prompt_shape
+    float* workspace;         // prompt_attention_bytes
+};
+PromptShape prompt_shape(int64_t tokens, int64_t sequences, int64_t heads, int64_t kv_heads, int64_t d, int64_t longest);
+size_t prompt_attention_bytes(const PromptShape& s, int64_t kv_heads, int64_t d);
+hipError_t launch_prompt_attention(const PromptAttention& a, hipStream_t stream);
 
 // ------------------------------------------------------------ device helpers
 

@@ -120,6 +120,21 @@ struct Unit {
     int at0, at1;
     bool turned;
     float cos[V], sin[V];
+
+    __device__ __forceinline__ void place(int u, int rot, bool interleaved)
+    {
+        turned = u < rot / (2 * V);
+        at0 = turned && !interleaved ? V * u : 2 * V * u;
+        at1 = turned && !interleaved ? at0 + rot / 2 : at0 + V;
+    }
+    __device__ __forceinline__ void angle(int i, int64_t freq, int32_t position, float magnitude, bool inverse)
+    {
+        const uint64_t turn = (uint64_t)freq * (uint64_t)(int64_t)position;
+        const float t = (float)(int32_t)(turn >> 32) * 0x1p-32f;
+        cos[i] = __builtin_amdgcn_cosf(t) * magnitude;
+        const float s = __builtin_amdgcn_sinf(t) * magnitude;
+        sin[i] = inverse ? -s : s;
+    }
 };
 
 template <int V>
@@ -127,23 +142,11 @@ __device__ __forceinline__ Unit<V> make_unit(int u, int rot, bool interleaved, i
                                              const int64_t* freqs, float magnitude, bool inverse)
 {
     Unit<V> w;
-    const int turned = rot / (2 * V);
-    w.turned = u < turned;
-    if (!w.turned) {
-        w.at0 = 2 * V * u;
-        w.at1 = w.at0 + V;
-        return w;
-    }
-    w.at0 = interleaved ? 2 * V * u : V * u;
-    w.at1 = interleaved ? w.at0 + V : w.at0 + rot / 2;
+    w.place(u, rot, interleaved);
+    if (w.turned)
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-        const uint64_t turn = (uint64_t)freqs[V * u + i] * (uint64_t)(int64_t)position;
-        const float t = (float)(int32_t)(turn >> 32) * 0x1p-32f;
-        w.cos[i] = __builtin_amdgcn_cosf(t) * magnitude;
-        const float s = __builtin_amdgcn_sinf(t) * magnitude;
-        w.sin[i] = inverse ? -s : s;
-    }
+        for (int i = 0; i < V; ++i)
+            w.angle(i, freqs[V * u + i], position, magnitude, inverse);
     return w;
 }
 
@@ -203,6 +206,102 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(const Rotary a, uint32
         const int64_t at = (int64_t)(first + i) * a.y_head;
         store<V>(y + at + w.at0, v0[i]);
         store<V>(y + at + w.at1, v1[i]);
+    }
+}
+
+// Norms of the heads of one token, turned by positions of one axis or several: y =
+// R(w x / sqrt(mean x^2 + eps)).  `lanes` lanes have a head's channels, units u, u +
+// lanes, ... of them each, and up to kHeadsPerThread heads, whose sums of squares
+// meet over the lanes; the queries' heads come first, the keys' behind them.
+// Sums, norms and rotations are fp32, with one rounding at the end.
+template <int V, int UNITS>
+__global__ __launch_bounds__(kThreads) void head_norm_kernel(const HeadNorm a, uint32_t lanes, uint32_t q_groups,
+                                                             uint32_t groups)
+{
+    const uint32_t id = blockIdx.x * kThreads + threadIdx.x;
+    const uint32_t rest = id / lanes, lane = id & (lanes - 1);
+    const uint32_t token = rest / groups, both = rest - token * groups;
+    const bool live = token < a.tokens, keys = both >= q_groups;
+    const HeadRows& r = keys ? a.k : a.q;
+    const int units = a.d / (2 * V), first = (int)(keys ? both - q_groups : both) * kHeadsPerThread;
+    Unit<V> w[UNITS];
+    float v0[kHeadsPerThread][UNITS][V], v1[kHeadsPerThread][UNITS][V], square[kHeadsPerThread];
+#pragma unroll
+    for (int j = 0; j < UNITS; ++j) {
+        const int u = (int)lane + j * (int)lanes;
+        const bool mine = live && u < units;
+        w[j].place(mine ? u : 0, a.rot, a.interleaved);
+#pragma unroll
+        for (int i = 0; i < kHeadsPerThread; ++i) {
+            const uint16_t* x = r.x + (int64_t)(live ? token : 0) * r.x_token + (int64_t)min(first + i, r.heads - 1) * r.x_head;
+            load<V>(x + w[j].at0, v0[i][j]);
+            load<V>(x + w[j].at1, v1[i][j]);
+            if (!mine)
+#pragma unroll
+                for (int c = 0; c < V; ++c)
+                    v0[i][j][c] = v1[i][j][c] = 0.0f;
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < UNITS; ++j) {
+        const int u = (int)lane + j * (int)lanes;
+        if (!w[j].turned || !live || u >= units)
+            continue;
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const int32_t axis = a.axes ? a.axes[V * u + i] : 0;
+            const int32_t position = axis >= 0 && axis < a.axis_count ? a.positions[axis * a.axis_stride + token] : 0;
+            w[j].angle(i, a.freqs[V * u + i], position, a.magnitude, false);
+        }
+    }
+    if (a.norm) {
+#pragma unroll
+        for (int i = 0; i < kHeadsPerThread; ++i) {
+            square[i] = 0.0f;
+#pragma unroll
+            for (int j = 0; j < UNITS; ++j)
+#pragma unroll
+                for (int c = 0; c < V; ++c)
+                    square[i] = __builtin_fmaf(v0[i][j][c], v0[i][j][c], __builtin_fmaf(v1[i][j][c], v1[i][j][c], square[i]));
+        }
+        for (uint32_t d = 1; d < lanes; d <<= 1)
+#pragma unroll
+            for (int i = 0; i < kHeadsPerThread; ++i)
+                square[i] += __shfl_xor(square[i], (int)d);
+#pragma unroll
+        for (int j = 0; j < UNITS; ++j) {
+            float w0[V], w1[V];
+#pragma unroll
+            for (int c = 0; c < V; ++c)
+                w0[c] = w1[c] = 1.0f;
+            if (r.weight) {
+                load<V>(r.weight + w[j].at0, w0);
+                load<V>(r.weight + w[j].at1, w1);
+            }
+#pragma unroll
+            for (int i = 0; i < kHeadsPerThread; ++i) {
+                const float by = 1.0f / __builtin_sqrtf(square[i] * a.inverse_d + a.eps);
+#pragma unroll
+                for (int c = 0; c < V; ++c) {
+                    v0[i][j][c] *= by * w0[c];
+                    v1[i][j][c] *= by * w1[c];
+                }
+            }
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < UNITS; ++j) {
+        if (!live || (int)lane + j * (int)lanes >= units)
+            continue;
+#pragma unroll
+        for (int i = 0; i < kHeadsPerThread; ++i) {
+            if (first + i >= r.heads)
+                break;
+            turn<V>(w[j], a.interleaved, v0[i][j], v1[i][j]);
+            uint16_t* y = r.y + (int64_t)token * r.y_token + (int64_t)(first + i) * r.y_head;
+            store<V>(y + w[j].at0, v0[i][j]);
+            store<V>(y + w[j].at1, v1[i][j]);
+        }
     }
 }
 
@@ -305,6 +404,32 @@ hipError_t launch_rotary(const Rotary& a, hipStream_t stream)
         rotary_kernel<2><<<grid, kThreads, 0, stream>>>(a, (uint32_t)units, (uint32_t)groups);
     else
         rotary_kernel<1><<<grid, kThreads, 0, stream>>>(a, (uint32_t)units, (uint32_t)groups);
+    return hipGetLastError();
+}
+
+hipError_t launch_head_norm(const HeadNorm& a, hipStream_t stream)
+{
+    const int64_t q_groups = (a.q.heads + kHeadsPerThread - 1) / kHeadsPerThread;
+    const int64_t groups = q_groups + (a.k.heads + kHeadsPerThread - 1) / kHeadsPerThread;
+    uintptr_t pointers = 0;
+    int64_t strides = 0;
+    for (const HeadRows* r : {&a.q, &a.k})
+        if (r->heads > 0) {
+            pointers |= reinterpret_cast<uintptr_t>(r->x) | reinterpret_cast<uintptr_t>(r->y) | reinterpret_cast<uintptr_t>(r->weight);
+            strides |= r->x_token | r->x_head | r->y_token | r->y_head;
+        }
+    const int v = vector_of(a.d, a.rot, pointers, strides), each = v == 8 ? 1 : v == 2 ? 2 : 4;
+    const int units = (a.d / (2 * v) + each - 1) / each;
+    uint32_t lanes = 1;
+    while ((int)lanes < units)
+        lanes *= 2;
+    const uint32_t grid = blocks_of(a.tokens * groups * lanes);
+    if (v == 8)
+        head_norm_kernel<8, 1><<<grid, kThreads, 0, stream>>>(a, lanes, (uint32_t)q_groups, (uint32_t)groups);
+    else if (v == 2)
+        head_norm_kernel<2, 2><<<grid, kThreads, 0, stream>>>(a, lanes, (uint32_t)q_groups, (uint32_t)groups);
+    else
+        head_norm_kernel<1, 4><<<grid, kThreads, 0, stream>>>(a, lanes, (uint32_t)q_groups, (uint32_t)groups);
     return hipGetLastError();
 }
 

@@ -1,5 +1,6 @@
 """The decoding step on 4-bit operands: MXFP4 quantization and linear layers, rotary positions,
-and attention of one new token a sequence over a paged cache (include/quartz.h, "decoding").
+and attention of one new token a sequence over a paged cache; head norms, attention of prompts and of
+drafted tokens' trees over the same cache (include/quartz.h, "decoding").
 
 As in the rest of the package, the functions named like the C entry points take raw integers and
 return the status code; the tensor helpers check their tensors (``ValueError``), allocate outputs on
@@ -34,6 +35,14 @@ _SIGNATURES = {
     "quartz_paged_attention_workspace_bytes": ([I64] * 7, SZ),
     "quartz_paged_attention": ([P, P] + [I64] * 8 + [P, P, I32, F32, F32, I64, I64, I64, P, I64, I64, P,
                                                      F32, I64, P, SZ, P], I32),
+    "quartz_head_norm_rotary": (([P, P] + [I64] * 5 + [P]) * 2 + [I64] * 3 + [P, I64, I64, P, P, I32, I32, F32, F32, P],
+                                I32),
+    "quartz_paged_prompt_workspace_bytes": ([I64] * 7, SZ),
+    "quartz_paged_prompt_attention": ([P, P] + [I64] * 9 + [P, P, I32, F32, F32, I64, I64, I64, P, I64, I64, P, P,
+                                                            F32, I64, F32, P, P, P, SZ, P], I32),
+    "quartz_paged_tree_attention": ([P, P] + [I64] * 9 + [P, P, I32, F32, F32, I64, I64, I64, P, I64, I64, P, P,
+                                                          P, I64, I64, F32, F32, P, SZ, P], I32),
+    "quartz_paged_keep": ([P, P, I64, I64, I64, P, P, I32] + [I64] * 5 + [P, I64, I64, P], I32),
 }
 
 
@@ -109,6 +118,48 @@ def quartz_paged_attention(q, o, sequences, heads, kv_heads, d, q_token, q_head,
                                             o_head, k_cache, v_cache, cache_type, k_scale, v_scale, pages,
                                             page_size, page_stride, table, table_pages, table_stride,
                                             lengths, scale, window, workspace, workspace_bytes, stream)
+
+
+def quartz_head_norm_rotary(q, q_out, q_heads, q_token, q_head, q_out_token, q_out_head, q_weight, k, k_out,
+                            k_heads, k_token, k_head, k_out_token, k_out_head, k_weight, tokens, d, rot, positions,
+                            axis_count, axis_stride, axes, freqs, layout, norm, eps, magnitude, stream) -> int:
+    return _q.load().quartz_head_norm_rotary(q, q_out, q_heads, q_token, q_head, q_out_token, q_out_head, q_weight,
+                                             k, k_out, k_heads, k_token, k_head, k_out_token, k_out_head, k_weight,
+                                             tokens, d, rot, positions, axis_count, axis_stride, axes, freqs, layout,
+                                             norm, eps, magnitude, stream)
+
+
+def quartz_paged_prompt_workspace_bytes(tokens, sequences, heads, kv_heads, d, page_size, table_pages) -> int:
+    return int(_q.load().quartz_paged_prompt_workspace_bytes(tokens, sequences, heads, kv_heads, d, page_size,
+                                                             table_pages))
+
+
+def quartz_paged_prompt_attention(q, o, tokens, sequences, heads, kv_heads, d, q_token, q_head, o_token, o_head,
+                                  k_cache, v_cache, cache_type, k_scale, v_scale, pages, page_size, page_stride,
+                                  table, table_pages, table_stride, starts, lengths, scale, window, cap, slopes,
+                                  prefix, workspace, workspace_bytes, stream) -> int:
+    return _q.load().quartz_paged_prompt_attention(q, o, tokens, sequences, heads, kv_heads, d, q_token, q_head,
+                                                   o_token, o_head, k_cache, v_cache, cache_type, k_scale, v_scale,
+                                                   pages, page_size, page_stride, table, table_pages, table_stride,
+                                                   starts, lengths, scale, window, cap, slopes, prefix, workspace,
+                                                   workspace_bytes, stream)
+
+
+def quartz_paged_tree_attention(q, o, tokens, sequences, heads, kv_heads, d, q_token, q_head, o_token, o_head,
+                                k_cache, v_cache, cache_type, k_scale, v_scale, pages, page_size, page_stride, table,
+                                table_pages, table_stride, starts, lengths, tree, tree_words, tree_stride, scale, cap,
+                                workspace, workspace_bytes, stream) -> int:
+    return _q.load().quartz_paged_tree_attention(q, o, tokens, sequences, heads, kv_heads, d, q_token, q_head,
+                                                 o_token, o_head, k_cache, v_cache, cache_type, k_scale, v_scale,
+                                                 pages, page_size, page_stride, table, table_pages, table_stride,
+                                                 starts, lengths, tree, tree_words, tree_stride, scale, cap,
+                                                 workspace, workspace_bytes, stream)
+
+
+def quartz_paged_keep(first, kept, sequences, most, kept_stride, k_cache, v_cache, cache_type, heads, d, pages,
+                      page_size, page_stride, table, table_pages, table_stride, stream) -> int:
+    return _q.load().quartz_paged_keep(first, kept, sequences, most, kept_stride, k_cache, v_cache, cache_type, heads,
+                                       d, pages, page_size, page_stride, table, table_pages, table_stride, stream)
 
 
 # ------------------------------------------------------------------- tensor helpers
@@ -292,3 +343,74 @@ def paged_attention(q, cache: PagedCache, lengths, scale: float | None = None, w
             return paged_attention(q, cache, lengths, scale, window, out, workspace)
     return _native().attention(cache.k, cache.v, cache.table, cache.k_scale, cache.v_scale, q, lengths, scale,
                                window, out, workspace)
+
+
+def head_norm_rotary(q, k, positions, freqs, q_weight=None, k_weight=None, eps: float | None = 1e-6, axes=None,
+                     layout: str = "half", magnitude: float = 1.0, out=None, stream=None):
+    """The heads of queries and keys (bf16 [tokens, heads, d], any token and head strides; ``k`` may be
+    None), each normed by its root mean square, scaled by its weight (bf16 [d]) and turned as by
+    ``rotary``, in one pass: returns both.  ``positions``: int32 [tokens], or [axes, tokens] for
+    positions of several axes, of which pair i takes axis ``axes[i]`` (int32 [len(freqs)]; frequencies
+    of each axis' own pairs one after the other).  ``eps=None``: turned only.  ``out``: a pair of
+    outputs (either may be None, or its input)."""
+    if stream is not None:
+        with _On(stream, q):
+            return head_norm_rotary(q, k, positions, freqs, q_weight, k_weight, eps, axes, layout, magnitude, out)
+    q_out, k_out = (None, None) if out is None else out
+    return _native().head_norm_rotary(q, k, positions, freqs, q_weight, k_weight, eps, axes, layout, magnitude,
+                                      q_out, k_out)
+
+
+def paged_prompt_workspace(tokens: int, heads: int, cache: PagedCache):
+    """Workspace of ``paged_prompt_attention`` and ``paged_tree_attention`` for these sizes, or None
+    where they need none."""
+    _, kv_heads, page, d = cache.k.shape
+    torch = _q._torch()
+    with torch.cuda.device(cache.k.device):      # sized for its compute units
+        n = quartz_paged_prompt_workspace_bytes(tokens, cache.table.shape[0], heads, kv_heads, d, page,
+                                                cache.table.shape[1])
+    return torch.empty((n,), dtype=torch.uint8, device=cache.k.device) if n else None
+
+
+def paged_prompt_attention(q, cache: PagedCache, starts, lengths, scale: float | None = None, window: int = 0,
+                           cap: float = 0.0, slopes=None, prefix=None, out=None, workspace=None, stream=None):
+    """Attention of the new tokens of prompts over their pages: q bf16 [tokens, heads, d] -> bf16
+    [tokens, heads, d].  Sequence b (a row of the table) has the tokens ``starts[b]`` to
+    ``starts[b + 1] - 1`` (int32 [sequences + 1]) at the last places of its ``lengths[b]`` (int32
+    [sequences]) keys, which ``paged_append`` has written before.  A token sees its own position and
+    those before it, the last ``window`` of them if that is set, and the first ``prefix[b]`` (int32
+    [sequences]) of its sequence.  ``cap`` caps scores, cap tanh(s / cap); ``slopes`` (fp32 [heads])
+    takes slope |distance| off them.  ``scale`` is 1 / sqrt(d) by default.  A token that sees nothing
+    gets zeros; rows of no sequence are left as they are."""
+    if stream is not None:
+        with _On(stream, q):
+            return paged_prompt_attention(q, cache, starts, lengths, scale, window, cap, slopes, prefix, out, workspace)
+    return _native().prompt_attention(cache.k, cache.v, cache.table, cache.k_scale, cache.v_scale, q, starts, lengths,
+                                      None, scale, window, cap, slopes, prefix, out, workspace)
+
+
+def paged_tree_attention(q, cache: PagedCache, starts, lengths, tree, scale: float | None = None, cap: float = 0.0,
+                         out=None, workspace=None, stream=None):
+    """Attention of trees of drafted tokens over their pages: as ``paged_prompt_attention``, but a token
+    sees every place before its sequence's new ones, and of those the ones whose bits are set in its
+    ``tree`` words (int64 [tokens, words]; bit i % 64 of word i // 64: the sequence's new token i, the
+    token itself among them).  The nodes of a tree lie in the cache's places one after the other,
+    whatever positions their keys were turned by; ``paged_keep`` moves the accepted ones."""
+    if stream is not None:
+        with _On(stream, q):
+            return paged_tree_attention(q, cache, starts, lengths, tree, scale, cap, out, workspace)
+    if tree is None:
+        raise ValueError("tree must be a tensor")
+    return _native().prompt_attention(cache.k, cache.v, cache.table, cache.k_scale, cache.v_scale, q, starts, lengths,
+                                      tree, scale, 0, cap, None, None, out, workspace)
+
+
+def paged_keep(cache: PagedCache, first, kept, stream=None) -> None:
+    """Moves the accepted tokens of trees to the places behind their sequences: place ``first[b] +
+    kept[b, i]`` to ``first[b] + i`` (int32 [sequences] and [sequences, most], a row of the table a
+    sequence), as if all were read before any is written.  Entries below i (-1 where there are no more)
+    move nothing."""
+    if stream is not None:
+        with _On(stream, cache.k):
+            return paged_keep(cache, first, kept)
+    _native().keep(cache.k, cache.v, cache.table, cache.k_scale, cache.v_scale, first, kept)
