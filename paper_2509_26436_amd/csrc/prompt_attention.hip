@@ -53,15 +53,15 @@ constexpr uint32_t kLeast = (127 - 24) << 7, kMost = (127 + 9) << 7;   // bf16 m
 constexpr float kUnits = 0x1p-7f;                // of O over the weights' sum
 
 // keys that a wave takes of a step, of a step, and the steps in shared memory
-constexpr int wave_keys(int kw) { return kw == 1 ? 64 : 32; }
-constexpr int step_keys(int kw) { return kw * wave_keys(kw); }
+constexpr int wave_keys(int d, int kw) { return kw == 1 && d < 256 ? 64 : 32; }
+constexpr int step_keys(int d, int kw) { return kw * wave_keys(d, kw); }
 constexpr int buffers(int kw) { return kw == 1 ? 2 : 1; }
 
 // Rows of shared memory: 16 bytes (V: 32, for the transposing reads) past the
 // channels, so that the rows an instruction reads lie in different banks.
 constexpr int k_pitch(int d) { return 2 * d + 16; }
 constexpr int v_pitch(int d) { return 2 * d + 32; }
-constexpr int buffer_bytes(int d, int kw) { return step_keys(kw) * (k_pitch(d) + v_pitch(d)); }
+constexpr int buffer_bytes(int d, int kw) { return step_keys(d, kw) * (k_pitch(d) + v_pitch(d)); }
 constexpr int merge_bytes(int d, int rw, int kw) { return kw == 1 ? 0 : rw * kw * 32 * (d + 4 + 2) * 4; }
 constexpr int shared_bytes(int d, int rw, int kw)
 {
@@ -105,11 +105,14 @@ __device__ __forceinline__ v16f mfma_half(v4u a, v4u b, v16f c)
 }
 
 // four keys of one channel each, from 4 keys x 16 channels of the 16 lanes around
-__device__ __forceinline__ v2u transposed(const uint8_t* p)
+typedef __attribute__((address_space(3))) const uint8_t* local_ptr;
+__device__ __forceinline__ v2u transposed(local_ptr p)
 {
-    return __builtin_bit_cast(v2u, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                                       (__attribute__((address_space(3))) s4*)(uintptr_t)(uint32_t)(uintptr_t)p));
+    return __builtin_bit_cast(v2u, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4*)p));
 }
+
+// the lowest n of 8 bits
+__device__ __forceinline__ uint32_t below(int n) { return (1u << min(max(n, 0), 8)) - 1; }
 
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
@@ -205,7 +208,7 @@ template <int D, bool FP8, int RW, int KW>
 __global__ __launch_bounds__(64 * RW * KW, (D == 256 ? 1 : 2)) void prompt_attention_kernel(const PromptAttention a)
 {
     constexpr int kThreads = 64 * RW * KW, kRows = 32 * RW;
-    constexpr int kWaveKeys = wave_keys(KW), kStep = step_keys(KW), kHalves = kWaveKeys / 32;
+    constexpr int kWaveKeys = wave_keys(D, KW), kStep = step_keys(D, KW), kHalves = kWaveKeys / 32;
     constexpr int kBuffers = buffers(KW);
     constexpr int kSteps = D / 16, kTiles = D / 32;
     constexpr int kBytes = FP8 ? 1 : 2;
@@ -276,7 +279,8 @@ __global__ __launch_bounds__(64 * RW * KW, (D == 256 ? 1 : 2)) void prompt_atten
     const uint8_t* v_at = static_cast<const uint8_t*>(c.v) + head_at * kBytes;
     const int32_t* table = c.table + (int64_t)tile.b * c.table_stride;
     const bool stages = kAll >= kThreads || (int)threadIdx.x < kAll;
-    int32_t pages[kMine], counts = 0, holes = 0;
+    int32_t pages[kMine];
+    uint32_t counts = 0, holes = 0;
     v4u kr[kMine], vr[kMine];
     auto key_of = [&](int i) { return (int)(threadIdx.x + i * kThreads) / kChunks; };
     const int chunk = (int)threadIdx.x % kChunks;
@@ -291,8 +295,8 @@ __global__ __launch_bounds__(64 * RW * KW, (D == 256 ? 1 : 2)) void prompt_atten
         for (int i = 0; i < kMine; ++i) {
             const int key = key0 + key_of(i);
             const bool is_page = pages[i] >= 0 && pages[i] < c.pages;
-            counts |= (is_page && key < tile.length ? 1 : 0) << i;
-            holes |= !is_page && key < tile.length ? 1 : 0;
+            counts |= (is_page && key < tile.length ? 1u : 0u) << i;
+            holes |= !is_page && key < tile.length ? 1u : 0u;
             const int64_t at = ((is_page ? pages[i] : 0) * c.page_stride + (int64_t)(key & mask) * D) * kBytes + 16 * chunk;
             if (stages) {
                 kr[i] = *reinterpret_cast<const v4u*>(k_at + at);
@@ -313,8 +317,8 @@ __global__ __launch_bounds__(64 * RW * KW, (D == 256 ? 1 : 2)) void prompt_atten
         for (int i = 0; i < kMine; ++i) {
             if (!stages)
                 break;
-            if (!(counts >> i & 1))
-                vr[i] = v4u{0, 0, 0, 0};
+            const uint32_t keep = counts >> i & 1 ? ~0u : 0u;
+            vr[i] &= v4u{keep, keep, keep, keep};
             uint8_t *kp = k_row(buffer, key_of(i)), *vp = v_row(buffer, key_of(i));
             if constexpr (FP8) {
                 v4u k0, k1, v0, v1;
@@ -448,19 +452,17 @@ __global__ __launch_bounds__(64 * RW * KW, (D == 256 ? 1 : 2)) void prompt_atten
 #pragma unroll
                     for (int t = 0; t < 2; ++t) {
                         const int run = key0 + 32 * x + 16 * t + 8 * h;          // 8 keys of one page
-                        uint32_t see = 0;
+                        uint32_t see;
                         if (a.tree) {
-#pragma unroll
-                            for (int j = 0; j < 8; ++j) {
-                                const int node = run + j - base;
-                                const bool past = node < 0;
-                                const bool bit = !past && node >> 6 < a.tree_words && (bits[min(max(node, 0) >> 6, a.tree_words - 1)] >> (node & 63) & 1);
-                                see |= ((past || bit) && run + j < sight.hi ? 1u : 0u) << j;
-                            }
+                            // the words around the run's first node; the past is all ones
+                            const int node = run - base, first = node >> 6, shift = node & 63;
+                            const uint64_t w0 = bits[min(max(first, 0), a.tree_words - 1)];
+                            const uint64_t w1 = bits[min(max(first + 1, 0), a.tree_words - 1)];
+                            const uint64_t lo = first < 0 ? ~0ull : first < a.tree_words ? w0 : 0;
+                            const uint64_t hi = first + 1 < 0 ? ~0ull : first + 1 < a.tree_words ? w1 : 0;
+                            see = (uint32_t)(lo >> shift | hi << 1 << (63 - shift)) & below(sight.hi - run);
                         } else {
-#pragma unroll
-                            for (int j = 0; j < 8; ++j)
-                                see |= ((run + j >= sight.lo && run + j < sight.hi) || run + j < sight.pre ? 1u : 0u) << j;
+                            see = (below(sight.hi - run) & ~below(sight.lo - run)) | below(sight.pre - run);
                         }
                         if (holed) {
                             const int32_t page = table[min(run >> c.page_shift, last_page)];
@@ -499,11 +501,10 @@ __global__ __launch_bounds__(64 * RW * KW, (D == 256 ? 1 : 2)) void prompt_atten
                 s[x][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[x][e], by, off));
         // V^T: 4 keys x 4 channels of a lane, whose rows are channels 16 h' + 4 a + i
         const int g = lane >> 4 & 1, piece = lane & 3;
-        const uint8_t* vp = buffer + kStep * k_pitch(D) + (mine + 8 * h + (lane >> 2 & 3)) * v_pitch(D) +
-                            2 * (16 * (piece & 1) + 4 * (2 * g + (piece >> 1)));
-        auto values = [&](int x, int t, int tile) {
-            const uint8_t* p = vp + (32 * x + 16 * t) * v_pitch(D) + 64 * tile;
-            const v2u lo = transposed(p), hi = transposed(p + 4 * v_pitch(D));
+        const local_ptr vp = (local_ptr)buffer + kStep * k_pitch(D) + (mine + 8 * h + (lane >> 2 & 3)) * v_pitch(D) +
+                             2 * (16 * (piece & 1) + 4 * (2 * g + (piece >> 1)));
+        auto values = [&](local_ptr p, int tile) {
+            const v2u lo = transposed(p + 64 * tile), hi = transposed(p + 64 * tile + 4 * v_pitch(D));
             return v4u{lo[0], lo[1], hi[0], hi[1]};
         };
         if (!slow) {
@@ -520,53 +521,77 @@ __global__ __launch_bounds__(64 * RW * KW, (D == 256 ? 1 : 2)) void prompt_atten
                     }
 #pragma unroll
                     for (int i = 0; i < kTiles; ++i)
-                        acc[i] = mfma_half(values(x, t, i), p, acc[i]);
+                        acc[i] = mfma_half(values(vp + (32 * x + 16 * t) * v_pitch(D), i), p, acc[i]);
                 }
-        } else {
+        }
+        // 16 keys at a time, in a loop: few steps need it.  Its count is opaque, since as the other
+        // branch of the above it would have a second set of O's registers.
+        int runs = slow ? 2 * kHalves : 0;
+        asm volatile("" : "+s"(runs));
+#pragma unroll 1
+        for (int run = 0; run < runs; ++run) {
+            float w[8];
 #pragma unroll
-            for (int x = 0; x < kHalves; ++x)
+            for (int j = 0; j < 8; ++j)
+                w[j] = s[0][j];
 #pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    v4u p, more, sees;
+            for (int r = 1; r < 2 * kHalves; ++r)
+                if (run == r)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        w[j] = s[r / 2][8 * (r % 2) + j];
+            v4u p, more;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                sum += w[2 * j] + w[2 * j + 1];
+                // the values lack their factor of 2^7
+                const float w0 = w[2 * j] * 0x1p7f, w1 = w[2 * j + 1] * 0x1p7f;
+                const uint32_t two = pack_bf16(w0, w1);
+                p[j] = two;
+                more[j] = pack_bf16(w0 - __uint_as_float(two << 16), w1 - __uint_as_float(two & 0xFFFF0000u));
+            }
+            const local_ptr at = vp + 16 * run * v_pitch(D);
+#pragma unroll
+            for (int i = 0; i < kTiles; ++i) {
+                v4u v = values(at, i);
+                if (special)
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        // the values lack their factor of 2^7
-                        const float w0 = s[x][8 * t + 2 * j] * 0x1p7f, w1 = s[x][8 * t + 2 * j + 1] * 0x1p7f;
-                        sum += s[x][8 * t + 2 * j] + s[x][8 * t + 2 * j + 1];
-                        p[j] = pack_bf16(w0, w1);
-                        more[j] = pack_bf16(w0 - __uint_as_float(p[j] << 16), w1 - __uint_as_float(p[j] & 0xFFFF0000u));
-                        const uint32_t two = seen >> (16 * x + 8 * t + 2 * j);
-                        sees[j] = (two & 1 ? 0x3F80u : 0u) | (two & 2 ? 0x3F800000u : 0u);
+                        const uint32_t w = v[j];
+                        v[j] = ((w & 0x7F80u) == 0x7F80u ? 0 : w & 0xFFFFu) |
+                               ((w & 0x7F800000u) == 0x7F800000u ? 0 : w & 0xFFFF0000u);
                     }
+                acc[i] = mfma_bf16(v, more, mfma_bf16(v, p, acc[i]));
+            }
+            if (!special)
+                continue;
+            // infinities of either sign and NaN, counted over the keys that the row sees
+            v4u sees;
 #pragma unroll
-                    for (int i = 0; i < kTiles; ++i) {
-                        const v4u raw = values(x, t, i);
-                        v4u v = raw;
-                        if (special)
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t two = seen >> (8 * run + 2 * j);
+                sees[j] = (two & 1 ? 0x3F80u : 0u) | (two & 2 ? 0x3F800000u : 0u);
+            }
+#pragma unroll 1
+            for (int kind = 0; kind < 3; ++kind) {
+                const uint32_t least = kind == 0 ? 0x7F80u : kind == 1 ? 0xFF80u : 0x7F81u;
+                const uint32_t last = kind == 2 ? 0x7FFFu : least, bits = kind == 2 ? 0x7FFFu : 0xFFFFu;
+                const float what = kind == 0 ? __builtin_inff() : kind == 1 ? -__builtin_inff() : __builtin_nanf("");
+                auto is = [&](uint32_t v) { return (v & bits) >= least && (v & bits) <= last; };
 #pragma unroll
-                            for (int j = 0; j < 4; ++j) {
-                                v[j] = (raw[j] & 0x7F80u) == 0x7F80u ? v[j] & 0xFFFF0000u : v[j];
-                                v[j] = (raw[j] & 0x7F800000u) == 0x7F800000u ? v[j] & 0xFFFFu : v[j];
-                            }
-                        acc[i] = mfma_bf16(v, more, mfma_bf16(v, p, acc[i]));
-                        if (special) {
-                            // infinities of either sign and NaN, counted over the keys that the row sees
-                            auto count = [&](auto is, float what) {
-                                v4u one;
+                for (int i = 0; i < kTiles; ++i) {
+                    v4u v = values(at, i);
 #pragma unroll
-                                for (int j = 0; j < 4; ++j)
-                                    one[j] = (is(raw[j] & 0xFFFFu) ? 0x3F80u : 0u) | (is(raw[j] >> 16) ? 0x3F800000u : 0u);
-                                const v16f found = mfma_bf16(one, sees, v16f{});
-#pragma unroll
-                                for (int e = 0; e < 16; ++e)
-                                    acc[i][e] += found[e] > 0.0f ? what : 0.0f;
-                            };
-                            count([](uint32_t v) { return v == 0x7F80u; }, __builtin_inff());
-                            count([](uint32_t v) { return v == 0xFF80u; }, -__builtin_inff());
-                            count([](uint32_t v) { return (v & 0x7FFFu) > 0x7F80u; }, __builtin_nanf(""));
-                        }
+                    for (int j = 0; j < 4; ++j) {
+                        const uint32_t w = v[j];
+                        v[j] = (is(w & 0xFFFFu) ? 0x3F80u : 0u) | (is(w >> 16) ? 0x3F800000u : 0u);
                     }
+                    const v16f found = mfma_bf16(v, sees, v16f{});
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+                        acc[i][e] += found[e] > 0.0f ? what : 0.0f;
                 }
+            }
         }
     };
 
@@ -707,7 +732,7 @@ hipError_t launch(const PromptAttention& a, hipStream_t stream)
     const uint32_t grid = (uint32_t)(a.tiles * a.splits * a.cache.heads);
     prompt_attention_kernel<D, FP8, RW, KW><<<grid, 64 * RW * KW, 0, stream>>>(a);
     if (a.splits > 1)
-        prompt_join_kernel<D, 32 * RW><<<dim3((uint32_t)(a.tiles * a.cache.heads), 32 * RW / (1024 / D)), 256, 0, stream>>>(a, step_keys(KW));
+        prompt_join_kernel<D, 32 * RW><<<dim3((uint32_t)(a.tiles * a.cache.heads), 32 * RW / (1024 / D)), 256, 0, stream>>>(a, step_keys(D, KW));
     return hipGetLastError();
 }
 
@@ -716,7 +741,9 @@ hipError_t launch(const PromptAttention& a, hipStream_t stream)
 {
     switch (a.rows) {
     case 32:
-        return launch<D, FP8, 1, 4>(a, stream);
+        if constexpr (D < 256)
+            return launch<D, FP8, 1, 4>(a, stream);
+        return hipErrorInvalidValue;
     case 64:
         return launch<D, FP8, 2, 2>(a, stream);
     case 128:
@@ -741,7 +768,7 @@ PromptShape prompt_shape(int64_t tokens, int64_t sequences, int64_t heads, int64
     const int64_t group = heads / kv_heads, rows = tokens * group;
     const int64_t each = (rows + sequences - 1) / sequences;
     PromptShape s;
-    s.rows = each <= 32 ? 32 : each <= 64 ? 64 : each <= 128 || d == 256 ? 128 : 256;
+    s.rows = each <= 32 && d < 256 ? 32 : each <= 64 ? 64 : each <= 128 || d == 256 ? 128 : 256;
     s.tiles = rows / s.rows + std::min(sequences, tokens);
     s.unit = 256;
     const int64_t parts = s.tiles * kv_heads, units = (longest + s.unit - 1) / s.unit;
