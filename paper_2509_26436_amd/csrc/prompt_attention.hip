@@ -57,10 +57,10 @@ constexpr int wave_keys(int d, int kw) { return kw == 1 && d < 256 ? 64 : 32; }
 constexpr int step_keys(int d, int kw) { return kw * wave_keys(d, kw); }
 constexpr int buffers(int kw) { return kw == 1 ? 2 : 1; }
 
-// Rows of shared memory: 16 bytes (V: 32, for the transposing reads) past the
+// Rows of shared memory: 16 bytes (V: 64, for the transposing reads) past the
 // channels, so that the rows an instruction reads lie in different banks.
 constexpr int k_pitch(int d) { return 2 * d + 16; }
-constexpr int v_pitch(int d) { return 2 * d + 32; }
+constexpr int v_pitch(int d) { return 2 * d + 64; }
 constexpr int buffer_bytes(int d, int kw) { return step_keys(d, kw) * (k_pitch(d) + v_pitch(d)); }
 constexpr int merge_bytes(int d, int rw, int kw) { return kw == 1 ? 0 : rw * kw * 32 * (d + 4 + 2) * 4; }
 constexpr int shared_bytes(int d, int rw, int kw)
@@ -413,13 +413,24 @@ __global__ __launch_bounds__(64 * RW * KW, (D == 256 ? 1 : 2)) void prompt_atten
         if (key0 >= any_hi || (key0 + kWaveKeys <= any_lo && key0 >= sight.pre))
             return;
         v16f s[kHalves];
-        const uint8_t* kp = buffer + (mine + n) * k_pitch(D) + 16 * h;
+        // reads of keys go kAhead instructions before the product that takes them
+        const local_ptr kp = (local_ptr)buffer + (mine + n) * k_pitch(D) + 16 * h;
+        constexpr int kProducts = kHalves * kSteps, kAhead = kProducts < 8 ? kProducts : 8;
+        v4u ring[kAhead];
+        auto key = [&](int j) {
+            return *(__attribute__((address_space(3))) const v4u*)(kp + 32 * (j % kHalves) * k_pitch(D) + 32 * (j / kHalves));
+        };
 #pragma unroll
-        for (int x = 0; x < kHalves; ++x) {
-            s[x] = v16f{};
+        for (int j = 0; j < kAhead; ++j)
+            ring[j] = key(j);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int i = 0; i < kSteps; ++i)
-                s[x] = mfma_bf16(*reinterpret_cast<const v4u*>(kp + 32 * x * k_pitch(D) + 32 * i), qf[i], s[x]);
+        for (int j = 0; j < kProducts; ++j) {
+            const int x = j % kHalves, i = j / kHalves;
+            s[x] = mfma_bf16(ring[j % kAhead], qf[i], i == 0 ? v16f{} : s[x]);
+            if (j + kAhead < kProducts)
+                ring[j % kAhead] = key(j + kAhead);
+            __builtin_amdgcn_sched_barrier(0);
         }
         const bool whole = !holed && ((key0 >= all_lo && key0 + kWaveKeys <= all_hi) || key0 + kWaveKeys <= sight.pre);
         uint32_t seen = 0xFFFFFFFFu;
@@ -508,22 +519,35 @@ __global__ __launch_bounds__(64 * RW * KW, (D == 256 ? 1 : 2)) void prompt_atten
             return v4u{lo[0], lo[1], hi[0], hi[1]};
         };
         if (!slow) {
+            v4u pp[2 * kHalves];
 #pragma unroll
             for (int x = 0; x < kHalves; ++x)
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
-                    v4u p;
+                    v4u& p = pp[2 * x + t];
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         const h2 two = __builtin_convertvector(f2{s[x][8 * t + 2 * j], s[x][8 * t + 2 * j + 1]}, h2);
                         sum = __builtin_amdgcn_fdot2(two, h2{1, 1}, sum, false);
                         p[j] = __builtin_bit_cast(uint32_t, two);
                     }
-#pragma unroll
-                    for (int i = 0; i < kTiles; ++i)
-                        acc[i] = mfma_half(values(vp + (32 * x + 16 * t) * v_pitch(D), i), p, acc[i]);
                 }
-        }
+            // reads of values go as far ahead
+            constexpr int kProducts = 2 * kHalves * kTiles, kAhead = kProducts < 8 ? kProducts : 8;
+            v4u ring[kAhead];
+            auto value = [&](int j) { return values(vp + 16 * (j / kTiles) * v_pitch(D), j % kTiles); };
+    #pragma unroll
+            for (int j = 0; j < kAhead; ++j)
+                ring[j] = value(j);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int j = 0; j < kProducts; ++j) {
+                acc[j % kTiles] = mfma_half(ring[j % kAhead], pp[j / kTiles], acc[j % kTiles]);
+                if (j + kAhead < kProducts)
+                    ring[j % kAhead] = value(j + kAhead);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            }
         // 16 keys at a time, in a loop: few steps need it.  Its count is opaque, since as the other
         // branch of the above it would have a second set of O's registers.
         int runs = slow ? 2 * kHalves : 0;
