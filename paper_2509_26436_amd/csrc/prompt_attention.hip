@@ -122,7 +122,7 @@ __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirs
 struct Tile {
     int first;                  // the sequence's first token
     int b, count, row0, rows;   // sequence, its tokens, this tile's rows of tokens x group
-    int length;                 // of its keys
+    int length, prefix;         // of its keys
 };
 
 // Tiles of all sequences one after the other, found by scanning their starts, which
@@ -134,30 +134,34 @@ __device__ __forceinline__ bool find_tile(const PromptAttention& a, int64_t inde
     for (int64_t b0 = 0; b0 < a.cache.sequences; b0 += 64) {
         const int64_t b = b0 + lane;
         int64_t s0 = 0, n = 0;
+        int length = 0, prefix = 0;
         if (b < a.cache.sequences) {
+            length = a.lengths[b];
+            prefix = a.prefix ? a.prefix[b] : 0;
             s0 = min(max((int64_t)a.starts[b], (int64_t)0), a.tokens);
             n = min(max((int64_t)a.starts[b + 1], s0), a.tokens) - s0;
         }
-        const int64_t mine = (n * group + rows - 1) / rows;
-        int64_t up = mine;
+        const int mine = (int)((n * group + rows - 1) / rows);       // 2^30 rows in all
+        int up = mine;
 #pragma unroll
         for (int d = 1; d < 64; d <<= 1) {
-            const int64_t other = __shfl_up(up, d);
+            const int other = __shfl_up(up, d);
             up += lane >= d ? other : 0;
         }
         const uint64_t past = __ballot(index < behind + up);
         if (past != 0) {
             const int at = __ffsll((unsigned long long)past) - 1;
-            t.b = uniform((int)(b0 + at));
-            t.first = uniform((int)__shfl(s0, at));
-            t.count = uniform((int)__shfl(n, at));
-            t.row0 = uniform((int)(index - behind - __shfl(up - mine, at)) * rows);
+            const auto of = [&](int v) { return __builtin_amdgcn_readlane(v, at); };
+            t.b = uniform((int)b0) + at;
+            t.first = of((int)s0);
+            t.count = of((int)n);
+            t.row0 = (int)(index - behind - of(up - mine)) * rows;
             t.rows = min(rows, t.count * group - t.row0);
-            const int64_t most = (int64_t)a.cache.table_pages << a.cache.page_shift;
-            t.length = uniform((int)min(max((int64_t)a.lengths[t.b], (int64_t)0), most));
+            t.length = (int)min(max((int64_t)of(length), (int64_t)0), (int64_t)a.cache.table_pages << a.cache.page_shift);
+            t.prefix = min(max(of(prefix), 0), t.length);
             return true;
         }
-        behind += __shfl(up, 63);
+        behind += __builtin_amdgcn_readlane(up, 63);
     }
     return false;
 }
@@ -167,11 +171,11 @@ __device__ __forceinline__ bool find_tile(const PromptAttention& a, int64_t inde
 struct Sight {
     int lo, hi, pre;
 };
-__device__ __forceinline__ Sight sight_of(const PromptAttention& a, const Tile& t, int i, int prefix)
+__device__ __forceinline__ Sight sight_of(const PromptAttention& a, const Tile& t, int i)
 {
     const int64_t end = (int64_t)t.length - t.count + i + 1;        // behind its own position
     Sight s;
-    s.pre = min(max(prefix, 0), t.length);
+    s.pre = t.prefix;
     if (a.tree) {
         s.hi = t.length;
         s.lo = 0;
@@ -186,9 +190,9 @@ __device__ __forceinline__ Sight sight_of(const PromptAttention& a, const Tile& 
 struct Keys {
     int from, to, behind_gap, unit, count;
 };
-__device__ __forceinline__ Keys keys_of(const PromptAttention& a, const Tile& t, int group, int step, int prefix)
+__device__ __forceinline__ Keys keys_of(const PromptAttention& a, const Tile& t, int group, int step)
 {
-    const Sight s0 = sight_of(a, t, t.row0 / group, prefix), s1 = sight_of(a, t, (t.row0 + t.rows - 1) / group, prefix);
+    const Sight s0 = sight_of(a, t, t.row0 / group), s1 = sight_of(a, t, (t.row0 + t.rows - 1) / group);
     Keys k;
     k.to = max(s1.hi, s0.pre);
     k.behind_gap = s0.lo & ~(step - 1);
@@ -230,8 +234,7 @@ __global__ __launch_bounds__(64 * RW * KW, (D == 256 ? 1 : 2)) void prompt_atten
     Tile tile;
     if (!find_tile(a, index, group, kRows, tile))
         return;
-    const int prefix = uniform(a.prefix ? a.prefix[tile.b] : 0);
-    const Keys keys = keys_of(a, tile, group, kStep, prefix);
+    const Keys keys = keys_of(a, tile, group, kStep);
     if (part >= max(keys.count, 1))
         return;
     const int first_key = keys.from + part * keys.unit;
@@ -242,7 +245,7 @@ __global__ __launch_bounds__(64 * RW * KW, (D == 256 ? 1 : 2)) void prompt_atten
     const bool live = row < tile.rows;
     const int at_row = tile.row0 + min(row, tile.rows - 1);
     const int token = at_row / group, head = kv * group + at_row % group;
-    Sight sight = sight_of(a, tile, token, prefix);
+    Sight sight = sight_of(a, tile, token);
     const int base = tile.length - tile.count;               // of a tree's nodes; may be negative
     const int position = base + token;
     const uint64_t* bits = a.tree ? a.tree + (int64_t)(tile.first + token) * a.tree_token : nullptr;
@@ -728,7 +731,7 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(const PromptAttention 
     if (!find_tile(a, index, group, ROWS, tile))
         return;
     const int row = blockIdx.y * kRows + (int)threadIdx.x / kLanes, channel = 4 * ((int)threadIdx.x % kLanes);
-    const Keys keys = keys_of(a, tile, group, step, uniform(a.prefix ? a.prefix[tile.b] : 0));
+    const Keys keys = keys_of(a, tile, group, step);
     if (row >= tile.rows || keys.count <= 1)
         return;
     v4f o = {};
@@ -794,10 +797,12 @@ PromptShape prompt_shape(int64_t tokens, int64_t sequences, int64_t heads, int64
     PromptShape s;
     s.rows = each <= 32 && d < 256 ? 32 : each <= 64 ? 64 : each <= 128 || d == 256 ? 128 : 256;
     s.tiles = rows / s.rows + std::min(sequences, tokens);
-    s.unit = 256;
-    const int64_t parts = s.tiles * kv_heads, units = (longest + s.unit - 1) / s.unit;
-    const int64_t want = (2 * device_compute_units() + parts - 1) / parts;
-    s.splits = (int)std::max<int64_t>(1, std::min<int64_t>({want, units, 64}));
+    s.unit = 512;
+    // blocks that the device holds, and tiles if no sequence leaves a part of one
+    const int64_t resident = device_compute_units() * (s.rows == 256 || d == 256 ? 1 : 2);
+    const int64_t parts = std::max((rows + s.rows - 1) / s.rows, std::min(sequences, tokens)) * kv_heads;
+    const int64_t units = (longest + s.unit - 1) / s.unit;
+    s.splits = (int)std::max<int64_t>(1, std::min<int64_t>({resident / parts, units, 64}));
     return s;
 }
 

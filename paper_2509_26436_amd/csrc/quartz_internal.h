@@ -326,6 +326,7 @@ struct HeadNorm {
     const int64_t* freqs;
     bool interleaved, norm;
     float magnitude, eps, inverse_d;
+    bool wide;                // frequencies and axes by 16 bytes
 };
 hipError_t launch_head_norm(const HeadNorm& a, hipStream_t stream);
 

@@ -224,6 +224,13 @@ __global__ __launch_bounds__(kThreads) void head_norm_kernel(const HeadNorm a, u
     const bool live = token < a.tokens, keys = both >= q_groups;
     const HeadRows& r = keys ? a.k : a.q;
     const int units = a.d / (2 * V), first = (int)(keys ? both - q_groups : both) * kHeadsPerThread;
+    // positions on the first axes; a load for each of a unit's pairs bound the kernel (queries and
+    // keys of 4608 tokens of 64 heads by three axes: 44.7 us, FIGURE so)
+    constexpr int kNear = 4;
+    int32_t near[kNear];
+#pragma unroll
+    for (int x = 0; x < kNear; ++x)
+        near[x] = a.rot > 0 && x < a.axis_count ? a.positions[x * a.axis_stride + (live ? token : 0)] : 0;
     Unit<V> w[UNITS];
     float v0[kHeadsPerThread][UNITS][V], v1[kHeadsPerThread][UNITS][V], square[kHeadsPerThread];
 #pragma unroll
@@ -247,11 +254,42 @@ __global__ __launch_bounds__(kThreads) void head_norm_kernel(const HeadNorm a, u
         const int u = (int)lane + j * (int)lanes;
         if (!w[j].turned || !live || u >= units)
             continue;
+        int64_t freqs[V];
+        int32_t axes[V];
+        if (V == 8 && a.wide) {
+#pragma unroll
+            for (int i = 0; i < V; i += 2) {
+                const longlong2 f = *reinterpret_cast<const longlong2*>(a.freqs + V * u + i);
+                freqs[i] = f.x;
+                freqs[i + (V > 1)] = f.y;
+            }
+            if (a.axes)
+#pragma unroll
+                for (int i = 0; i < V; i += 4) {
+                    const int4 x = *reinterpret_cast<const int4*>(a.axes + V * u + i);
+                    axes[i] = x.x;
+                    axes[(i + 1) % V] = x.y;
+                    axes[(i + 2) % V] = x.z;
+                    axes[(i + 3) % V] = x.w;
+                }
+        } else {
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                freqs[i] = a.freqs[V * u + i];
+                if (a.axes)
+                    axes[i] = a.axes[V * u + i];
+            }
+        }
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            const int32_t axis = a.axes ? a.axes[V * u + i] : 0;
-            const int32_t position = axis >= 0 && axis < a.axis_count ? a.positions[axis * a.axis_stride + token] : 0;
-            w[j].angle(i, a.freqs[V * u + i], position, a.magnitude, false);
+            const int32_t axis = a.axes ? axes[i] : 0;
+            int32_t position = 0;                // of an axis that is none
+#pragma unroll
+            for (int x = 0; x < kNear; ++x)
+                position = axis == x ? near[x] : position;
+            if (a.axis_count > kNear && axis >= kNear && axis < a.axis_count)
+                position = a.positions[axis * a.axis_stride + token];
+            w[j].angle(i, freqs[i], position, a.magnitude, false);
         }
     }
     if (a.norm) {
@@ -407,8 +445,10 @@ hipError_t launch_rotary(const Rotary& a, hipStream_t stream)
     return hipGetLastError();
 }
 
-hipError_t launch_head_norm(const HeadNorm& a, hipStream_t stream)
+hipError_t launch_head_norm(const HeadNorm& given, hipStream_t stream)
 {
+    HeadNorm a = given;
+    a.wide = ((reinterpret_cast<uintptr_t>(a.freqs) | reinterpret_cast<uintptr_t>(a.axes)) & 15) == 0;
     const int64_t q_groups = (a.q.heads + kHeadsPerThread - 1) / kHeadsPerThread;
     const int64_t groups = q_groups + (a.k.heads + kHeadsPerThread - 1) / kHeadsPerThread;
     uintptr_t pointers = 0;
