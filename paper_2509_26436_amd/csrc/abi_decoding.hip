@@ -28,6 +28,8 @@ constexpr float kMinValueScale = 0x1p-96f;
 constexpr int64_t kMaxNorm = 512;
 // query rows of one call of several tokens a sequence
 constexpr int64_t kMaxRows = int64_t(1) << 30;
+// channels of a call's sequences that tokens are kept of: 2^25 columns of 16 bytes, 2^21 blocks of 16
+constexpr int64_t kMaxKept = int64_t(1) << 31;
 // caps of scores: the tanh is off by 2e-7, times the cap
 constexpr float kMinCap = 0x1p-10f, kMaxCap = 1024.0f;
 
@@ -456,7 +458,8 @@ quartz_status quartz_paged_keep(const int32_t* first, const int32_t* kept, int64
 {
     if (sequences < 0 || most < 0 || most > kMaxPositions || heads <= 0 || heads > kMaxK ||
         kept_stride < most || kept_stride > kMaxStride || !product_ok(sequences, heads, kMaxBlocks512) ||
-        d <= 0 || d > kMaxK || table_pages < 0 || table_pages > kMaxPositions)
+        d <= 0 || d > kMaxK || !product_ok(sequences, heads * d, kMaxKept) || table_pages < 0 ||
+        table_pages > kMaxPositions)
         return QUARTZ_ERR_SHAPE;
     PagedKeep a{};
     a.cache = {k_cache, v_cache, pages, page_stride, (int32_t)heads, (int32_t)d, shift_of(page_size),
@@ -533,6 +536,8 @@ static quartz_status prompt_attention(PromptAttention a, const void* q_bf16, voi
         !aligned16(workspace) || ((q_token | q_head) & 7) != 0 || ((o_token | o_head) & 3) != 0)
         return QUARTZ_ERR_ALIGN;
     const PromptShape s = prompt_shape(tokens, sequences, heads, kv_heads, d, table_pages * page_size);
+    if (!product_ok(s.tiles * s.splits, kv_heads, kMaxBlocks512))
+        return QUARTZ_ERR_SHAPE;
     const size_t need = prompt_attention_bytes(s, kv_heads, d);
     if (need > 0 && (!workspace || workspace_bytes < need))
         return QUARTZ_ERR_WORKSPACE;
