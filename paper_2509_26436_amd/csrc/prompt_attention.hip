@@ -52,21 +52,33 @@ constexpr uint32_t kValue = 7;                   // values in fp16 times 2^7
 constexpr uint32_t kLeast = (127 - 24) << 7, kMost = (127 + 9) << 7;   // bf16 magnitudes that fp16 takes
 constexpr float kUnits = 0x1p-7f;                // of O over the weights' sum
 
-// keys that a wave takes of a step, of a step, and the steps in shared memory
-constexpr int wave_keys(int d, int kw) { return kw == 1 && d < 256 ? 64 : 32; }
-constexpr int step_keys(int d, int kw) { return kw * wave_keys(d, kw); }
+// Keys that a wave takes of a step, and keys of a step.  Where the memory bounds the
+// call larger steps keep more of it on the way: 32 sequences of 5 to 26 nodes over 129
+// to 4096 e4m3 keys 81.3 us with 32 keys a wave, 73.5 with 64; 9 to 16 nodes over as
+// many bf16 keys of 64 channels 62.6, 53.1, of 128 (whose steps are in the registers
+// then) 90.0, 110.8.
+constexpr int wave_keys(int d, bool fp8, int kw)
+{
+    return (kw == 1 && d < 256) || (kw == 2 && (d == 64 || (d == 128 && fp8))) ? 64 : 32;
+}
+constexpr int step_keys(int d, bool fp8, int kw) { return kw * wave_keys(d, fp8, kw); }
+// steps in shared memory
 constexpr int buffers(int kw) { return kw == 1 ? 2 : 1; }
 
 // Rows of shared memory: 16 bytes (V: 64, for the transposing reads) past the
 // channels, so that the rows an instruction reads lie in different banks.
 constexpr int k_pitch(int d) { return 2 * d + 16; }
 constexpr int v_pitch(int d) { return 2 * d + 64; }
-constexpr int buffer_bytes(int d, int kw) { return step_keys(d, kw) * (k_pitch(d) + v_pitch(d)); }
+constexpr int buffer_bytes(int d, bool fp8, int kw) { return step_keys(d, fp8, kw) * (k_pitch(d) + v_pitch(d)); }
 constexpr int merge_bytes(int d, int rw, int kw) { return kw == 1 ? 0 : rw * kw * 32 * (d + 4 + 2) * 4; }
-constexpr int shared_bytes(int d, int rw, int kw)
+constexpr int shared_bytes(int d, bool fp8, int rw, int kw)
 {
-    return std::max(buffers(kw) * buffer_bytes(d, kw), merge_bytes(d, rw, kw));
+    return std::max(buffers(kw) * buffer_bytes(d, fp8, kw), merge_bytes(d, rw, kw));
 }
+// Blocks of four waves that a compute unit's registers hold.  One row of waves over bf16
+// keys of 128 channels wants all of them: 128 sequences of 2 to 7 nodes over 1000 to 4096
+// keys 346 us with two blocks, 326 with one (4.1 TB/s; e4m3, which does not, 154, 228).
+constexpr int blocks_fit(int d, bool fp8, int rw) { return d == 256 || (d == 128 && !fp8 && rw == 1) ? 1 : 2; }
 
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b)
 {
@@ -209,16 +221,16 @@ __device__ __forceinline__ float* parts_o(const PromptAttention& a, int64_t slot
 }
 
 template <int D, bool FP8, int RW, int KW>
-__global__ __launch_bounds__(64 * RW * KW, (D == 256 ? 1 : 2)) void prompt_attention_kernel(const PromptAttention a)
+__global__ __launch_bounds__(64 * RW * KW, blocks_fit(D, FP8, RW)) void prompt_attention_kernel(const PromptAttention a)
 {
     constexpr int kThreads = 64 * RW * KW, kRows = 32 * RW;
-    constexpr int kWaveKeys = wave_keys(D, KW), kStep = step_keys(D, KW), kHalves = kWaveKeys / 32;
+    constexpr int kWaveKeys = wave_keys(D, FP8, KW), kStep = step_keys(D, FP8, KW), kHalves = kWaveKeys / 32;
     constexpr int kBuffers = buffers(KW);
     constexpr int kSteps = D / 16, kTiles = D / 32;
     constexpr int kBytes = FP8 ? 1 : 2;
     constexpr int kChunks = D * kBytes / 16;                 // 16-byte pieces of a key
     constexpr int kAll = kStep * kChunks, kMine = (kAll + kThreads - 1) / kThreads;
-    __shared__ __align__(16) uint8_t shared[shared_bytes(D, RW, KW)];
+    __shared__ __align__(16) uint8_t shared[shared_bytes(D, FP8, RW, KW)];
     __shared__ int marks[kBuffers][4];                       // step a buffer was found so in: slow, special, holes
 
     const PagedCacheView& c = a.cache;
@@ -313,7 +325,7 @@ __global__ __launch_bounds__(64 * RW * KW, (D == 256 ? 1 : 2)) void prompt_atten
     auto v_row = [&](uint8_t* buffer, int key) { return buffer + kStep * k_pitch(D) + key * v_pitch(D); };
     // stores what fetch() got; `found` marks the buffer's step where values need bf16
     auto store = [&](int slot, int found) {
-        uint8_t* buffer = shared + slot * buffer_bytes(D, KW);
+        uint8_t* buffer = shared + slot * buffer_bytes(D, FP8, KW);
         uint32_t out = 0, top = 0;                           // (e4m3: out)
         us2 least = {0xFFFF, 0xFFFF}, most = {0, 0};
 #pragma unroll
@@ -374,7 +386,7 @@ __global__ __launch_bounds__(64 * RW * KW, (D == 256 ? 1 : 2)) void prompt_atten
             marks[slot][2] = found;
     };
     auto store_values = [&](int slot) {                      // as bf16
-        uint8_t* buffer = shared + slot * buffer_bytes(D, KW);
+        uint8_t* buffer = shared + slot * buffer_bytes(D, FP8, KW);
 #pragma unroll
         for (int i = 0; i < kMine; ++i) {
             if (!stages)
@@ -410,7 +422,7 @@ __global__ __launch_bounds__(64 * RW * KW, (D == 256 ? 1 : 2)) void prompt_atten
 
     // one step's product of a wave with its 32 or 64 keys
     auto compute = [&](int slot, int key0, bool slow, bool special, bool holed) {
-        const uint8_t* buffer = shared + slot * buffer_bytes(D, KW);
+        const uint8_t* buffer = shared + slot * buffer_bytes(D, FP8, KW);
         const int mine = kw * kWaveKeys;
         key0 += mine;
         if (key0 >= any_hi || (key0 + kWaveKeys <= any_lo && key0 >= sight.pre))
@@ -759,7 +771,7 @@ hipError_t launch(const PromptAttention& a, hipStream_t stream)
     const uint32_t grid = (uint32_t)(a.tiles * a.splits * a.cache.heads);
     prompt_attention_kernel<D, FP8, RW, KW><<<grid, 64 * RW * KW, 0, stream>>>(a);
     if (a.splits > 1)
-        prompt_join_kernel<D, 32 * RW><<<dim3((uint32_t)(a.tiles * a.cache.heads), 32 * RW / (1024 / D)), 256, 0, stream>>>(a, step_keys(D, KW));
+        prompt_join_kernel<D, 32 * RW><<<dim3((uint32_t)(a.tiles * a.cache.heads), 32 * RW / (1024 / D)), 256, 0, stream>>>(a, step_keys(D, FP8, KW));
     return hipGetLastError();
 }
 
