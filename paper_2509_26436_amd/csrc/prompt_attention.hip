@@ -14,8 +14,8 @@
 //     the 16 scores that a lane gets, of one query, are two runs of 8 keys: its
 //     share of P^T in the next product, without an exchange.
 //   O^T = V^T P^T: V^T comes out of shared memory by transposing reads.
-// The softmax runs along with a running maximum (kept while scores are at most 2^8
-// above it) and fp32 sums.
+// The softmax runs along with a running maximum (kept while weights are at most 2^8
+// above one: moved at every step 8 ragged prompts take 188 us for 173) and fp32 sums.
 //
 // P enters the product in 16 bits.  In fp16, times 2^7, a weight is off by 2^-11 of
 // itself down to 2^-21 of the largest one, where bf16 would leave 2^-8, and V is
@@ -23,7 +23,18 @@
 // 2^-24 <= |v| < 2^9 (e4m3: any number).  A step with another value keeps bf16
 // values and takes the weights in two bf16 parts (2^-16), and counts infinities and
 // NaN apart, for the rows that see them only: a weight of zero times either would
-// reach rows that do not.
+// reach rows that do not.  All steps so: 952 us for 674 (8192 tokens of 32 heads of 128
+// channels), 263 for 173 (8 ragged prompts over e4m3).
+//
+// What bounds it: long prompts the issue of instructions.  8192 tokens of 32 heads take
+// 650 us, 846 TFLOP/s, where a large matrix product of the library reaches 1230; the
+// matrix unit is busy for 31 % of the cycles at 2.3 GHz.  A step of 64 keys and 32 rows
+// has 32 products (36 cycles each, 16 of which keep vector instructions out) beside some
+// 250 vector instructions (16 maxima, 32 products, 32 exponentials, 16 roundings, 16 sums,
+// 64 for the values' turn to fp16), and its two waves a SIMD, which a barrier a step
+// holds together, are in the same part of it at a time.  Trees over long caches are
+// bound by the memory (128 of 2 to 7 nodes over bf16 keys 4.1 TB/s), short calls by
+// the latencies of starts, pages and keys.
 #include <algorithm>
 #include <cfloat>
 #include <climits>
@@ -127,6 +138,13 @@ __device__ __forceinline__ v2u transposed(local_ptr p)
 __device__ __forceinline__ uint32_t below(int n) { return (1u << min(max(n, 0), 8)) - 1; }
 
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+
+// Parts of a tile's keys at most, and more than which teams of threads join: 8 nodes of
+// 8 heads over 100000 keys 60.2 us with 64 parts that a thread joins one after the
+// other, 36.5 with 128 and 29.2 with 256 that teams do; over 8000 e4m3 keys of two
+// cache heads 18.3 and 14.9.
+constexpr int64_t kMostParts = 256;
+constexpr int kManyParts = 16;
 
 // ---- the list of tiles
 
@@ -730,26 +748,27 @@ __global__ __launch_bounds__(64 * RW * KW, blocks_fit(D, FP8, RW)) void prompt_a
     }
 }
 
-// Joins the parts of tiles whose keys several blocks took: a thread four channels of
-// a row.
-template <int D, int ROWS>
+// Joins the parts of tiles whose keys several blocks took.  A thread has four channels of
+// a row; TEAMS: of every kTeams-th part of it, which meet in shared memory.
+template <int D, int ROWS, bool TEAMS>
 __global__ __launch_bounds__(256) void prompt_join_kernel(const PromptAttention a, int step)
 {
-    constexpr int kLanes = D / 4, kRows = 256 / kLanes;
+    constexpr int kLanes = D / 4, kTeams = 256 / kLanes;
     const PagedCacheView& c = a.cache;
     const int group = a.heads / c.heads, kv = (int)(blockIdx.x % (uint32_t)c.heads);
     const int64_t index = blockIdx.x / (uint32_t)c.heads;
     Tile tile;
     if (!find_tile(a, index, group, ROWS, tile))
         return;
-    const int row = blockIdx.y * kRows + (int)threadIdx.x / kLanes, channel = 4 * ((int)threadIdx.x % kLanes);
+    const int team = (int)threadIdx.x / kLanes, lane = (int)threadIdx.x % kLanes, channel = 4 * lane;
+    const int row = TEAMS ? blockIdx.y : blockIdx.y * kTeams + team;
     const Keys keys = keys_of(a, tile, group, step);
     if (row >= tile.rows || keys.count <= 1)
-        return;
+        return;                                  // with TEAMS the whole block
     v4f o = {};
     float high = kNoScore, l = 0.0f;
 #pragma unroll 4
-    for (int i = 0; i < keys.count; ++i) {
+    for (int i = TEAMS ? team : 0; i < keys.count; i += TEAMS ? kTeams : 1) {
         const float* from = parts_o(a, (index * c.heads + kv) * a.splits + i, ROWS, D);
         const f2 ml = *reinterpret_cast<const f2*>(from + (int64_t)ROWS * D + 2 * row);
         const v4f part = *reinterpret_cast<const v4f*>(from + (int64_t)row * D + channel);
@@ -758,6 +777,29 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(const PromptAttention 
         o = o * keep + part * by;
         l = l * keep + ml[1] * by;
         high = next;
+    }
+    if constexpr (TEAMS) {
+        __shared__ v4f sums[kTeams][kLanes];
+        __shared__ float tops[kTeams], weights[kTeams];
+        sums[team][lane] = o;
+        if (lane == 0) {
+            tops[team] = high;
+            weights[team] = l;
+        }
+        __syncthreads();
+        if (team != 0)
+            return;
+#pragma unroll
+        for (int i = 1; i < kTeams; ++i)
+            high = fmaxf(high, tops[i]);
+        o = v4f{};
+        l = 0.0f;
+#pragma unroll
+        for (int i = 0; i < kTeams; ++i) {
+            const float by = __builtin_amdgcn_exp2f(tops[i] - high);
+            o += sums[i][lane] * by;
+            l += weights[i] * by;
+        }
     }
     const float by = l == 0.0f ? 0.0f : kUnits / l;
     const int at = tile.row0 + row;
@@ -770,8 +812,14 @@ hipError_t launch(const PromptAttention& a, hipStream_t stream)
 {
     const uint32_t grid = (uint32_t)(a.tiles * a.splits * a.cache.heads);
     prompt_attention_kernel<D, FP8, RW, KW><<<grid, 64 * RW * KW, 0, stream>>>(a);
-    if (a.splits > 1)
-        prompt_join_kernel<D, 32 * RW><<<dim3((uint32_t)(a.tiles * a.cache.heads), 32 * RW / (1024 / D)), 256, 0, stream>>>(a, step_keys(D, FP8, KW));
+    if (a.splits > 1) {
+        const uint32_t tiles = (uint32_t)(a.tiles * a.cache.heads), rows = 32 * RW;
+        constexpr int kStep = step_keys(D, FP8, KW);
+        if (a.splits > kManyParts)
+            prompt_join_kernel<D, 32 * RW, true><<<dim3(tiles, rows), 256, 0, stream>>>(a, kStep);
+        else
+            prompt_join_kernel<D, 32 * RW, false><<<dim3(tiles, rows / (1024 / D)), 256, 0, stream>>>(a, kStep);
+    }
     return hipGetLastError();
 }
 
@@ -807,14 +855,24 @@ PromptShape prompt_shape(int64_t tokens, int64_t sequences, int64_t heads, int64
     const int64_t group = heads / kv_heads, rows = tokens * group;
     const int64_t each = (rows + sequences - 1) / sequences;
     PromptShape s;
+    // As many rows as a sequence has, since a tile reads all of its keys and turns their
+    // values: 8192 tokens of 32 heads 650 us with 256 rows, 750 with 128, 8 ragged prompts
+    // over e4m3 169, 184; 1 to 8 drafted tokens of 32 heads 14.8 with 32 rows, 15.5 with 64,
+    // 20.7 with 128.  (256 channels: 128 rows are a block's registers, 32 would be too few
+    // for what is on its way.)
     s.rows = each <= 32 && d < 256 ? 32 : each <= 64 ? 64 : each <= 128 || d == 256 ? 128 : 256;
     s.tiles = rows / s.rows + std::min(sequences, tokens);
-    s.unit = 512;
-    // blocks that the device holds, and tiles if no sequence leaves a part of one
+    // Parts of at least four steps or so; short sequences are one: 1000 tokens of 8 heads
+    // 27.3 us with 256 keys a part, 33.1 with 512; 1 to 8 tokens over 341 keys 15.1 in two
+    // parts, 13.6 in one.
+    s.unit = longest > 512 ? 256 : 512;
+    // As many as the device holds at once (tiles counted as if no sequence left a part of
+    // one): 64 nodes of 64 heads over 131000 keys 357 us with 16 parts of each of 16 tiles,
+    // 389 with 32, 485 with 22, which leave a second round that is almost empty.
     const int64_t resident = device_compute_units() * (s.rows == 256 || d == 256 ? 1 : 2);
     const int64_t parts = std::max((rows + s.rows - 1) / s.rows, std::min(sequences, tokens)) * kv_heads;
     const int64_t units = (longest + s.unit - 1) / s.unit;
-    s.splits = (int)std::max<int64_t>(1, std::min<int64_t>({resident / parts, units, 64}));
+    s.splits = (int)std::max<int64_t>(1, std::min<int64_t>({resident / parts, units, kMostParts}));
     return s;
 }
 
