@@ -184,6 +184,39 @@ def test_scores_that_rise(rise):
     T.check(o, x, R.host(k), R.host(v), tab, [0, 70], lengths, page, scale=1.0)
 
 
+@pytest.mark.parametrize("d,new", [(64, 5), (128, 100), (256, 60)])
+def test_smallest_values_that_fp16_takes(d, new):
+    """Values that are subnormal in fp16, all of them: taken exactly, not lost."""
+    import torch
+    kv, group, page, lengths = 1, 4, 16, [300, 130]
+    g, tab, k, v, x, cache = _case(16, [new, new], lengths, kv, group, d, page, False)
+    vh = R.bf16(np.exp2(g.uniform(-24, -21.1, R.host(v).shape)) * g.choice([-1.0, 1.0], R.host(v).shape))
+    vh = np.where(np.abs(vh) < 2.0 ** -24, 2.0 ** -24, vh)
+    v.copy_(torch.from_numpy(vh).cuda().to(torch.bfloat16))
+    o = _run(x, cache, [new, new], lengths)
+    T.check(o, x, R.host(k), R.host(v), tab, T.starts_of([new, new]), lengths, page)
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("new", [3, 100])
+@pytest.mark.parametrize("below", [10.0, 17.25, 21.0])
+def test_many_weights_far_below_the_largest(below, new, fp8):
+    """One key takes nearly all the weight and has the value 0: the rest, e^-below each, is what is left."""
+    import torch
+    kv, group, d, page, lengths = 1, 2, 64, 16, [900]
+    _, tab, k, v, x, cache = _case(17, [new], lengths, kv, group, d, page, fp8)
+    kh, vh = np.zeros(R.host(k).shape), np.ones(R.host(v).shape)
+    kh[..., 0] = -below if not fp8 else -round(below)
+    kh[tab[0, 1], 0, 3, 0], vh[tab[0, 1], 0, 3] = 0.0, 0.0
+    for t, h in ((k, kh), (v, vh)):
+        t.copy_(torch.from_numpy(h).cuda().to(torch.bfloat16).to(t.dtype))
+    x[:] = 0.0
+    x[:, :, 0] = 1.0
+    o = _run(x, cache, [new], lengths, scale=1.0)
+    T.check(o, x, R.host(k), R.host(v), tab, [0, new], lengths, page, scale=1.0)
+    assert (o > 0).all()
+
+
 def test_views_and_rows_of_nobody():
     """Strided queries, outputs and caches; rows before the first, behind the last sequence stay."""
     import torch
