@@ -866,13 +866,26 @@ PromptShape prompt_shape(int64_t tokens, int64_t sequences, int64_t heads, int64
     // 27.3 us with 256 keys a part, 33.1 with 512; 1 to 8 tokens over 341 keys 15.1 in two
     // parts, 13.6 in one.
     s.unit = longest > 512 ? 256 : 512;
-    // As many as the device holds at once (tiles counted as if no sequence left a part of
-    // one): 64 nodes of 64 heads over 131000 keys 357 us with 16 parts of each of 16 tiles,
-    // 389 with 32, 485 with 22, which leave a second round that is almost empty.
+    // As many as the device holds at once (tiles counted as if all sequences were alike): 64
+    // nodes of 64 heads over 131000 keys 357 us with 16 parts of each of 16 tiles, 389 with
+    // 32, 485 with 22, which leave a second round that is almost empty.
     const int64_t resident = device_compute_units() * (s.rows == 256 || d == 256 ? 1 : 2);
-    const int64_t parts = std::max((rows + s.rows - 1) / s.rows, std::min(sequences, tokens)) * kv_heads;
-    const int64_t units = (longest + s.unit - 1) / s.unit;
-    s.splits = (int)std::max<int64_t>(1, std::min<int64_t>({resident / parts, units, kMostParts}));
+    const int64_t parts = std::min(sequences, tokens) * ((each + s.rows - 1) / s.rows) * kv_heads;
+    const int64_t units = std::min((longest + s.unit - 1) / s.unit, kMostParts);
+    s.splits = (int)std::max<int64_t>(1, std::min(resident / parts, units));
+    // More of them where that leaves compute units without a tile: rounds of blocks, of some
+    // 2.2 us for 64 keys, beside what a join reads and writes.  17 trees of 24 to 48 nodes
+    // over 3200 to 6000 e4m3 keys (136 tiles of 256 rows) 185 us in one part each, 130 so.
+    if (parts < resident) {
+        const auto expected = [&](int64_t splits) {
+            const int64_t rounds = (parts * splits + resident - 1) / resident;
+            return (double)rounds / splits * longest * (2.2 / 64) +
+                   (splits > 1 ? 5.0 + (double)parts * splits * s.rows * (d + 2) * 8 / 5e6 : 0.0);
+        };
+        for (int64_t splits = s.splits + 1; splits <= std::min<int64_t>(units, 4 * s.splits); ++splits)
+            if (expected(splits) < expected(s.splits))
+                s.splits = (int)splits;
+    }
     return s;
 }
 
