@@ -732,8 +732,8 @@ quartz_status quartz_paged_attention(const void* q_bf16, void* o_bf16, int64_t s
  *   starts     int32 [sequences + 1]: sequence b has the tokens starts[b] ..
  *              starts[b + 1] - 1 (rows of q and o), at the last positions of its
  *              lengths[b] (int32 [sequences]) keys, which hold them already.  Starts
- *              are clamped to [0, tokens] and lengths to the table; rows of no
- *              sequence are neither read nor written.
+ *              must not fall; they are clamped to [0, tokens] and lengths to the
+ *              table; rows of no sequence are neither read nor written.
  *   A token at position p sees the positions j <= p, the last `window` of them if
  *   that is set, and those below prefix[b] (int32 [sequences], NULL: none) of its
  *   sequence.
@@ -747,9 +747,9 @@ quartz_status quartz_paged_attention(const void* q_bf16, void* o_bf16, int64_t s
  *
  * Of both: q, o, scales, cache and table as for quartz_paged_attention, o zero where
  * a token sees no key or only scores of -inf.  What the cache holds in places that a
- * token does not see does not matter to it.  Weights hold 11 bits beside bf16 values
- * that fp16 takes (0 or 2^-24 <= |v| < 2^9) or e4m3 ones, else 16; sums are fp32,
- * of values times 2^14.  workspace: quartz_paged_prompt_workspace_bytes, as for
+ * token does not see does not matter to it.  Weights hold 11 bits (down to
+ * 2^-21 of a row's largest) beside bf16 values that fp16 takes (0 or 2^-24 <= |v| <
+ * 2^9) or e4m3 ones, else 16; sums are fp32, of values times 2^14.  workspace: quartz_paged_prompt_workspace_bytes, as for
  * quartz_paged_attention.  The host reads no starts or lengths: a call may be captured
  * into a graph and replayed with others.
  *

@@ -37,7 +37,6 @@
 // the latencies of starts, pages and keys.
 #include <algorithm>
 #include <cfloat>
-#include <climits>
 
 #include "quartz_internal.h"
 
@@ -249,7 +248,8 @@ __global__ __launch_bounds__(64 * RW * KW, blocks_fit(D, FP8, RW)) void prompt_a
     constexpr int kChunks = D * kBytes / 16;                 // 16-byte pieces of a key
     constexpr int kAll = kStep * kChunks, kMine = (kAll + kThreads - 1) / kThreads;
     __shared__ __align__(16) uint8_t shared[shared_bytes(D, FP8, RW, KW)];
-    __shared__ int marks[kBuffers][4];                       // step a buffer was found so in: slow, special, holes
+    // steps whose values need bf16, hold infinities or NaN, whose keys lack pages: their numbers
+    __shared__ int marks[kBuffers][4];
 
     const PagedCacheView& c = a.cache;
     const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
@@ -344,7 +344,7 @@ __global__ __launch_bounds__(64 * RW * KW, blocks_fit(D, FP8, RW)) void prompt_a
     // stores what fetch() got; `found` marks the buffer's step where values need bf16
     auto store = [&](int slot, int found) {
         uint8_t* buffer = shared + slot * buffer_bytes(D, FP8, KW);
-        uint32_t out = 0, top = 0;                           // (e4m3: out)
+        uint32_t out = 0;                                    // bits of e4m3 NaN
         us2 least = {0xFFFF, 0xFFFF}, most = {0, 0};
 #pragma unroll
         for (int i = 0; i < kMine; ++i) {
@@ -392,7 +392,7 @@ __global__ __launch_bounds__(64 * RW * KW, blocks_fit(D, FP8, RW)) void prompt_a
         if constexpr (FP8) {
             slow = special = (out & 0x80808080u) != 0;
         } else {
-            top = max(most[0], most[1]);
+            const uint32_t top = max(most[0], most[1]);
             special = top >= 0x7F80u;
             slow = top >= kMost || min(least[0], least[1]) < kLeast - 1;
         }
