@@ -5,16 +5,20 @@
 // kColumns of a sequence's, and kEntries entries at a time: all their rows are read,
 // then all are written.  kept[i] > i where anything moves, so a source is never a row
 // that an earlier entry has written, and the entries of later turns find theirs as
-// they were before the call.  Bound by latency (entry, pages, row), not by memory: 256
-// sequences of up to 128 entries (8 heads of 128 e4m3 channels, 68 MB) took 69 us
-// with eight rows of a column on their way and 23 us so (2.9 TB/s); a few entries of
-// 64 sequences 4.4, a launch.
+// they were before the call.  Bound by the memory where there are many: 256 sequences of
+// up to 128 entries (8 heads of 128 e4m3 channels, 34 MB each way) take 15 us, 4.5 TB/s.
+// For that the eight rows of a thread have to be on their way together, without a branch
+// between their loads and in registers: one after the other through scratch memory, as
+// an array of uint4 lies, they take 31 us and twice the bytes.  A few entries of 64
+// sequences 4.4, a launch.
 #include <algorithm>
 
 #include "quartz_internal.h"
 
 namespace quartz {
 namespace {
+
+typedef uint32_t v4u __attribute__((ext_vector_type(4)));     // (an array of uint4 would lie in scratch memory)
 
 constexpr int kThreads = 256;
 constexpr int kColumns = 16;
@@ -43,27 +47,34 @@ __global__ __launch_bounds__(kThreads) void paged_keep_kernel(const PagedKeep a,
     };
     for (int64_t i0 = 0; i0 < a.most; i0 += kEntries) {
         __syncthreads();
+        int64_t source = -1, target = -1;
         if (threadIdx.x < kEntries) {
             const int64_t i = i0 + threadIdx.x, node = i < a.most ? a.kept[b * a.kept_stride + i] : -1;
-            int64_t source = -1, target = -1;
             if (node > i) {
                 source = place(first + node);
                 target = place(first + i);
             }
-            from[threadIdx.x] = target < 0 ? -1 : source;
+            if (source < 0)
+                target = -1;
+            from[threadIdx.x] = target < 0 ? 0 : source;
             to[threadIdx.x] = target;
         }
+        if (!__syncthreads_or(target >= 0))
+            continue;
+        // There is a page: entries that do not move read its first row, which nothing uses,
+        // so that no branch stands between the loads.
+        v4u w[kFlight];
+#pragma unroll
+        for (int j = 0; j < kFlight; ++j)
+            w[j] = *reinterpret_cast<const v4u*>(at + from[team + j * kTeams]);
+        // Every row has been read before one is written: the barrier alone would not wait
+        // for loads that are on their way.
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
-        uint4 w[kFlight];
 #pragma unroll
         for (int j = 0; j < kFlight; ++j)
-            if (mine && from[team + j * kTeams] >= 0)
-                w[j] = *reinterpret_cast<const uint4*>(at + from[team + j * kTeams]);
-        __syncthreads();                                      // every row has been read (its load waited for)
-#pragma unroll
-        for (int j = 0; j < kFlight; ++j)
-            if (mine && from[team + j * kTeams] >= 0)
-                *reinterpret_cast<uint4*>(at + to[team + j * kTeams]) = w[j];
+            if (mine && to[team + j * kTeams] >= 0)
+                *reinterpret_cast<v4u*>(at + to[team + j * kTeams]) = w[j];
     }
 }
 

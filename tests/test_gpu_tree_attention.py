@@ -155,6 +155,27 @@ def test_keep_nothing():
     assert torch.equal(k, want) and torch.equal(v, want)
 
 
+@pytest.mark.parametrize("moved", [(), (0,), (1,), (2,), (0, 2)])
+@pytest.mark.parametrize("fp8", [False, True])
+def test_keep_runs_that_stay(moved, fp8):
+    """384 entries, of which whole runs of 128 stay where they are; in the others each source is the
+    next entry's target, and one sequence has no pages at all."""
+    import torch
+    import paper_2509_26436_amd as q
+    g = T.rng(8)
+    page, kv, d, most = 16, 2, 128, 384
+    tab, pages = T.table(g, [most + 40] * 3, page)
+    tab[1] = -1
+    k, v = T.cache(g, pages, kv, page, d, fp8)
+    kept = np.tile(np.arange(most), (3, 1))
+    for run in moved:
+        kept[:, 128 * run:128 * run + 128] += 1
+    raw = torch.uint8 if fp8 else torch.int16
+    want = [_moved(t.view(raw), tab, [3, 3, 30], kept, page, pages) for t in (k, v)]
+    q.paged_keep(q.PagedCache(k, v, T.int32(tab)), T.int32([3, 3, 30]), T.int32(kept))
+    assert torch.equal(k.view(raw), want[0]) and torch.equal(v.view(raw), want[1])
+
+
 # ------------------------------------------------------------------- together
 
 @pytest.mark.parametrize("captured", [False, True])
