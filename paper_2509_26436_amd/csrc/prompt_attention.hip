@@ -57,6 +57,10 @@ typedef unsigned short us2 __attribute__((ext_vector_type(2)));
 
 constexpr float kNoScore = -FLT_MAX;             // a maximum no score is below, finite
 constexpr float kSlack = 8.0f;                   // scores above the maximum before it moves (log2)
+// Maxima past which a step's scores are rounded as the maximum was before it is taken off
+// them.  Below, scores go into the exponential with their factor in one instruction, off by
+// the roundings of the maximum, less than 2^-3; past 2^24 those could pass what fp16 holds.
+constexpr float kLarge = 0x1p20f;
 constexpr float kWeight = 7.0f;                  // weights are held times 2^7
 constexpr uint32_t kValue = 7;                   // values in fp16 times 2^7
 constexpr uint32_t kLeast = (127 - 24) << 7, kMost = (127 + 9) << 7;   // bf16 magnitudes that fp16 takes
@@ -437,6 +441,7 @@ __global__ __launch_bounds__(64 * RW * KW, blocks_fit(D, FP8, RW)) void prompt_a
     for (int t = 0; t < kTiles; ++t)
         acc[t] = v16f{};
     float top = kNoScore, sum = 0.0f;
+    bool large = true;                                       // a row's maximum is past kLarge, or none yet
 
     // one step's product of a wave with its 32 or 64 keys
     auto compute = [&](int slot, int key0, bool slow, bool special, bool holed) {
@@ -528,16 +533,26 @@ __global__ __launch_bounds__(64 * RW * KW, blocks_fit(D, FP8, RW)) void prompt_a
         most *= by;
         const f2 both = halves(most);
         most = fmaxf(both[0], both[1]);
-        if (__any(most > top + kSlack)) {
+        if (__any(most - top > kSlack)) {
             const float next = fmaxf(most, top);
             const float keep = __builtin_amdgcn_exp2f(top - next);
             top = next;
+            large = __any(__builtin_fabsf(top) > kLarge);
             sum *= keep;
 #pragma unroll
             for (int t = 0; t < kTiles; ++t)
                 acc[t] *= keep;
         }
-        const float off = kWeight - top;
+        float off = kWeight - top;
+        if (large) {
+#pragma unroll
+            for (int x = 0; x < kHalves; ++x)
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    s[x][e] = s[x][e] * by - top;
+            by = 1.0f;
+            off = kWeight;
+        }
 #pragma unroll
         for (int x = 0; x < kHalves; ++x)
 #pragma unroll
