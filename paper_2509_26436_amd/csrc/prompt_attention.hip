@@ -24,7 +24,10 @@
 // values and takes the weights in two bf16 parts (2^-16), and counts infinities and
 // NaN apart, for the rows that see them only: a weight of zero times either would
 // reach rows that do not.  All steps so: 952 us for 674 (8192 tokens of 32 heads of 128
-// channels), 263 for 173 (8 ragged prompts over e4m3).
+// channels), 263 for 173 (8 ragged prompts over e4m3).  O's sums are of up to 2^22
+// times a value and key, so a block that meets a value of 2^64 or more starts over:
+// all its steps are such then, and the weights of n keys at most 1 / n, which no
+// value is too large for.
 //
 // What bounds it: long prompts the issue of instructions.  8192 tokens of 32 heads take
 // 650 us, 846 TFLOP/s, where a large matrix product of the library reaches 1230; the
@@ -61,10 +64,12 @@ constexpr float kSlack = 8.0f;                   // scores above the maximum bef
 // them.  Below, scores go into the exponential with their factor in one instruction, off by
 // the roundings of the maximum, less than 2^-3; past 2^24 those could pass what fp16 holds.
 constexpr float kLarge = 0x1p20f;
+constexpr int kNoKey = 1 << 30;                  // behind all of a sequence's
 constexpr float kWeight = 7.0f;                  // weights are held times 2^7
 constexpr uint32_t kValue = 7;                   // values in fp16 times 2^7
 constexpr uint32_t kLeast = (127 - 24) << 7, kMost = (127 + 9) << 7;   // bf16 magnitudes that fp16 takes
 constexpr float kUnits = 0x1p-7f;                // of O over the weights' sum
+constexpr uint32_t kHuge = (127 + 64) << 7;      // bf16 magnitudes whose sums could pass fp32's range
 
 // Keys that a wave takes of a step, and keys of a step.  Where the memory bounds the
 // call larger steps keep more of it on the way: 32 sequences of 5 to 26 nodes over 129
@@ -252,8 +257,9 @@ __global__ __launch_bounds__(64 * RW * KW, blocks_fit(D, FP8, RW)) void prompt_a
     constexpr int kChunks = D * kBytes / 16;                 // 16-byte pieces of a key
     constexpr int kAll = kStep * kChunks, kMine = (kAll + kThreads - 1) / kThreads;
     __shared__ __align__(16) uint8_t shared[shared_bytes(D, FP8, RW, KW)];
-    // steps whose values need bf16, hold infinities or NaN, whose keys lack pages: their numbers
-    __shared__ int marks[kBuffers][4];
+    // steps whose keys lack pages, whose values need bf16, and of these the ones that hold infinities or
+    // NaN, or huge values (or either): their numbers
+    __shared__ __align__(16) int marks[kBuffers][4];
 
     const PagedCacheView& c = a.cache;
     const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
@@ -392,20 +398,24 @@ __global__ __launch_bounds__(64 * RW * KW, blocks_fit(D, FP8, RW)) void prompt_a
                 *reinterpret_cast<v4u*>(vp + 16 * chunk) = v;
             }
         }
-        bool slow, special;
+        bool slow, special, huge = false;
         if constexpr (FP8) {
             slow = special = (out & 0x80808080u) != 0;
         } else {
             const uint32_t top = max(most[0], most[1]);
             special = top >= 0x7F80u;
             slow = top >= kMost || min(least[0], least[1]) < kLeast - 1;
+            huge = top >= kHuge;
         }
-        if (slow)
-            marks[slot][0] = found;
-        if (special)
-            marks[slot][1] = found;
         if (holes)
-            marks[slot][2] = found;
+            marks[slot][0] = found;
+        if (slow) {
+            marks[slot][1] = found;
+            if (special)
+                marks[slot][2] = found;
+            if (huge)
+                marks[slot][3] = found;
+        }
     };
     auto store_values = [&](int slot) {                      // as bf16
         uint8_t* buffer = shared + slot * buffer_bytes(D, FP8, KW);
@@ -442,6 +452,11 @@ __global__ __launch_bounds__(64 * RW * KW, blocks_fit(D, FP8, RW)) void prompt_a
         acc[t] = v16f{};
     float top = kNoScore, sum = 0.0f;
     bool large = true;                                       // a row's maximum is past kLarge, or none yet
+    // A value is huge: the weights of fewer than 2^power keys are at most 2^-power in the product, and the
+    // maximum moves at once.
+    bool huge = false;
+    const int power = 32 - __clz(max(end_key - first_key, 1));
+    const float low = __uint_as_float(uniform(__float_as_uint((float)(-7 - power))));
 
     // one step's product of a wave with its 32 or 64 keys
     auto compute = [&](int slot, int key0, bool slow, bool special, bool holed) {
@@ -533,7 +548,7 @@ __global__ __launch_bounds__(64 * RW * KW, blocks_fit(D, FP8, RW)) void prompt_a
         most *= by;
         const f2 both = halves(most);
         most = fmaxf(both[0], both[1]);
-        if (__any(most - top > kSlack)) {
+        if (__any(most - top > (huge ? 0.0f : kSlack))) {
             const float next = fmaxf(most, top);
             const float keep = __builtin_amdgcn_exp2f(top - next);
             top = next;
@@ -543,7 +558,8 @@ __global__ __launch_bounds__(64 * RW * KW, blocks_fit(D, FP8, RW)) void prompt_a
             for (int t = 0; t < kTiles; ++t)
                 acc[t] *= keep;
         }
-        float off = kWeight - top;
+        const float unit = huge ? low : kWeight;
+        float off = unit - top;
         if (large) {
 #pragma unroll
             for (int x = 0; x < kHalves; ++x)
@@ -551,7 +567,7 @@ __global__ __launch_bounds__(64 * RW * KW, blocks_fit(D, FP8, RW)) void prompt_a
                 for (int e = 0; e < 16; ++e)
                     s[x][e] = s[x][e] * by - top;
             by = 1.0f;
-            off = kWeight;
+            off = unit;
         }
 #pragma unroll
         for (int x = 0; x < kHalves; ++x)
@@ -678,14 +694,24 @@ __global__ __launch_bounds__(64 * RW * KW, blocks_fit(D, FP8, RW)) void prompt_a
         int slot = 0, found = 1;
         for (int key0 = first_key; key0 < end_key; ++found) {
             __syncthreads();
-            const bool slow = __builtin_amdgcn_readfirstlane(marks[slot][0]) == found;
-            const bool special = __builtin_amdgcn_readfirstlane(marks[slot][1]) == found;
-            const bool holed = __builtin_amdgcn_readfirstlane(marks[slot][2]) == found;
-            if (slow) {
+            const int4 mark = *reinterpret_cast<const int4*>(marks[slot]);
+            const bool holed = uniform(mark.x) == found, special = uniform(mark.z) == found;
+            bool slow = uniform(mark.y) == found;
+            int next = behind(key0);
+            if (huge | slow) {
+                slow = true;
+                if (!FP8 && !huge & (uniform(mark.w) == found)) {
+                    // the block starts over; the first maximum of a row takes what the row has to nothing
+                    huge = large = true;
+                    top = kNoScore;
+                    sum = 0.0f;
+                    key0 = kNoKey;
+                    next = first_key;
+                    find(next);
+                }
                 store_values(slot);
                 __syncthreads();
             }
-            const int next = behind(key0);
             if (next < end_key) {
                 fetch(next);
                 find(behind(next));
@@ -708,16 +734,18 @@ __global__ __launch_bounds__(64 * RW * KW, blocks_fit(D, FP8, RW)) void prompt_a
     }
     float* const slots = parts_o(a, (index * c.heads + kv) * a.splits + part, kRows, D);
     const bool last = keys.count <= 1;
+    const float weight = huge ? __builtin_amdgcn_ldexpf(0x1p14f, power) : 1.0f;
+    // a part leaves its mean and the sum of its weights times 2^7
     auto write = [&](int row, int channel, v4f o, float top, float sum) {
+        o *= sum == 0.0f ? 0.0f : kUnits / sum;
         if (last) {
             const int at = tile.row0 + row;
-            const float by = sum == 0.0f ? 0.0f : kUnits / sum;
             uint16_t* to = a.o + (int64_t)(tile.first + at / group) * a.o_token + (int64_t)(kv * group + at % group) * a.o_head + channel;
-            *reinterpret_cast<uint2*>(to) = output(o * by * c.v_scale);
+            *reinterpret_cast<uint2*>(to) = output(o * c.v_scale);
         } else {
             *reinterpret_cast<v4f*>(slots + (int64_t)row * D + channel) = o;
             if (channel == 0)
-                *reinterpret_cast<f2*>(slots + (int64_t)kRows * D + 2 * row) = f2{top, sum};
+                *reinterpret_cast<f2*>(slots + (int64_t)kRows * D + 2 * row) = f2{top, sum * weight};
         }
     };
     if constexpr (KW == 1) {
@@ -763,8 +791,9 @@ __global__ __launch_bounds__(64 * RW * KW, blocks_fit(D, FP8, RW)) void prompt_a
     }
 }
 
-// Joins the parts of tiles whose keys several blocks took.  A thread has four channels of
-// a row; TEAMS: of every kTeams-th part of it, which meet in shared memory.
+// Joins the parts of tiles whose keys several blocks took: the mean of their means, a
+// mean at every step, which no value is too large for.  A thread has four channels of a
+// row; TEAMS: of every kTeams-th part of it, which meet in shared memory.
 template <int D, int ROWS, bool TEAMS>
 __global__ __launch_bounds__(256) void prompt_join_kernel(const PromptAttention a, int step)
 {
@@ -788,9 +817,10 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(const PromptAttention 
         const f2 ml = *reinterpret_cast<const f2*>(from + (int64_t)ROWS * D + 2 * row);
         const v4f part = *reinterpret_cast<const v4f*>(from + (int64_t)row * D + channel);
         const float next = fmaxf(high, ml[0]);
-        const float keep = __builtin_amdgcn_exp2f(high - next), by = __builtin_amdgcn_exp2f(ml[0] - next);
-        o = o * keep + part * by;
-        l = l * keep + ml[1] * by;
+        const float old = l * __builtin_amdgcn_exp2f(high - next), more = ml[1] * __builtin_amdgcn_exp2f(ml[0] - next);
+        l = old + more;
+        const float by = l == 0.0f ? 0.0f : __builtin_amdgcn_rcpf(l);
+        o = o * (old * by) + part * (more * by);
         high = next;
     }
     if constexpr (TEAMS) {
@@ -807,19 +837,19 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(const PromptAttention 
 #pragma unroll
         for (int i = 1; i < kTeams; ++i)
             high = fmaxf(high, tops[i]);
-        o = v4f{};
         l = 0.0f;
 #pragma unroll
-        for (int i = 0; i < kTeams; ++i) {
-            const float by = __builtin_amdgcn_exp2f(tops[i] - high);
-            o += sums[i][lane] * by;
-            l += weights[i] * by;
-        }
+        for (int i = 0; i < kTeams; ++i)
+            l += weights[i] * __builtin_amdgcn_exp2f(tops[i] - high);
+        const float by = l == 0.0f ? 0.0f : 1.0f / l;
+        o = v4f{};
+#pragma unroll
+        for (int i = 0; i < kTeams; ++i)
+            o += sums[i][lane] * (weights[i] * __builtin_amdgcn_exp2f(tops[i] - high) * by);
     }
-    const float by = l == 0.0f ? 0.0f : kUnits / l;
     const int at = tile.row0 + row;
     uint16_t* to = a.o + (int64_t)(tile.first + at / group) * a.o_token + (int64_t)(kv * group + at % group) * a.o_head + channel;
-    *reinterpret_cast<uint2*>(to) = output(o * by * c.v_scale);
+    *reinterpret_cast<uint2*>(to) = output(o * c.v_scale);
 }
 
 template <int D, bool FP8, int RW, int KW>
