@@ -751,7 +751,8 @@ quartz_status quartz_paged_attention(const void* q_bf16, void* o_bf16, int64_t s
  * row's largest) beside bf16 values that fp16 takes (0 or 2^-24 <= |v| < 2^9) or e4m3
  * ones, else 16; sums are fp32, and finite where scores and values are (beside a value
  * of 2^64 or more, weights below 2^-88 of a row's largest may count as none and values
- * below 2^-95 lose bits).  workspace: quartz_paged_prompt_workspace_bytes, as for
+ * below 2^-95 lose bits); an infinite value is in the answer of every token that sees
+ * it, whatever its weight.  workspace: quartz_paged_prompt_workspace_bytes, as for
  * quartz_paged_attention.  The host reads no starts or lengths: a call may be captured
  * into a graph and replayed with others.
  *

@@ -142,6 +142,18 @@ __device__ __forceinline__ v2u transposed(local_ptr p)
     return __builtin_bit_cast(v2u, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4*)p));
 }
 
+// A value times a weight of a row that sees it: infinities stay, also where the weight is below
+// fp32's numbers (of two NaN and a number the median is the number).
+__device__ __forceinline__ float weighed(float v, float by)
+{
+    const float w = v * by;
+    return __builtin_amdgcn_fmed3f(w, w, v);
+}
+__device__ __forceinline__ v4f weighed(v4f v, float by)
+{
+    return v4f{weighed(v[0], by), weighed(v[1], by), weighed(v[2], by), weighed(v[3], by)};
+}
+
 // the lowest n of 8 bits
 __device__ __forceinline__ uint32_t below(int n) { return (1u << min(max(n, 0), 8)) - 1; }
 
@@ -554,9 +566,20 @@ __global__ __launch_bounds__(64 * RW * KW, blocks_fit(D, FP8, RW)) void prompt_a
             top = next;
             large = __any(__builtin_fabsf(top) > kLarge);
             sum *= keep;
+            // a loop of none or one (as for the slow product, below)
+            int infinities = !FP8 && huge ? 1 : 0;
+            asm volatile("" : "+s"(infinities));
+#pragma unroll 1
+            for (; infinities > 0; --infinities)
+#pragma unroll
+                for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+                        acc[t][e] = weighed(acc[t][e], keep);
+            const float rest = !FP8 && huge ? 1.0f : keep;
 #pragma unroll
             for (int t = 0; t < kTiles; ++t)
-                acc[t] *= keep;
+                acc[t] *= rest;
         }
         const float unit = huge ? low : kWeight;
         float off = unit - top;
@@ -783,7 +806,8 @@ __global__ __launch_bounds__(64 * RW * KW, blocks_fit(D, FP8, RW)) void prompt_a
 #pragma unroll
             for (int w = 0; w < KW; ++w) {
                 const float by = __builtin_amdgcn_exp2f(ml[w][0] - high);
-                o += *reinterpret_cast<const v4f*>(from[w] + (row % 32) * kRow + channel) * by;
+                const v4f part = *reinterpret_cast<const v4f*>(from[w] + (row % 32) * kRow + channel);
+                o += FP8 ? part * by : weighed(part, by);
                 l += ml[w][1] * by;
             }
             write(row, channel, o, high, l);
@@ -820,7 +844,7 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(const PromptAttention 
         const float old = l * __builtin_amdgcn_exp2f(high - next), more = ml[1] * __builtin_amdgcn_exp2f(ml[0] - next);
         l = old + more;
         const float by = l == 0.0f ? 0.0f : __builtin_amdgcn_rcpf(l);
-        o = o * (old * by) + part * (more * by);
+        o = weighed(o, old * by) + weighed(part, more * by);
         high = next;
     }
     if constexpr (TEAMS) {
@@ -845,7 +869,7 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(const PromptAttention 
         o = v4f{};
 #pragma unroll
         for (int i = 0; i < kTeams; ++i)
-            o += sums[i][lane] * (weights[i] * __builtin_amdgcn_exp2f(tops[i] - high) * by);
+            o += weighed(sums[i][lane], weights[i] * __builtin_amdgcn_exp2f(tops[i] - high) * by);
     }
     const int at = tile.row0 + row;
     uint16_t* to = a.o + (int64_t)(tile.first + at / group) * a.o_token + (int64_t)(kv * group + at % group) * a.o_head + channel;
