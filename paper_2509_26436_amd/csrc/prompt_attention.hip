@@ -951,7 +951,8 @@ PromptShape prompt_shape(int64_t tokens, int64_t sequences, int64_t heads, int64
             return (double)rounds / splits * longest * (2.2 / 64) +
                    (splits > 1 ? 5.0 + (double)parts * splits * s.rows * (d + 2) * 8 / 5e6 : 0.0);
         };
-        for (int64_t splits = s.splits + 1; splits <= std::min<int64_t>(units, 4 * s.splits); ++splits)
+        const int64_t most = std::min<int64_t>(units, 4 * s.splits);
+        for (int64_t splits = s.splits + 1; splits <= most; ++splits)
             if (expected(splits) < expected(s.splits))
                 s.splits = (int)splits;
     }
