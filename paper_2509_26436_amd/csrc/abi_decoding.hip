@@ -14,8 +14,9 @@ using namespace quartz;
 
 namespace {
 
-// blocks of 512 threads whose grid stays below 2^32 threads
+// blocks of 512 (256) threads whose grid stays below 2^32 threads
 constexpr int64_t kMaxBlocks512 = (int64_t(1) << 23) - 1;
+constexpr int64_t kMaxBlocks256 = (int64_t(1) << 24) - 1;
 // elements of one rotary (append) call: below 2^32 threads of one pair each
 constexpr int64_t kMaxRotary = int64_t(1) << 32;
 constexpr int64_t kMaxAppend = int64_t(1) << 31;
@@ -28,8 +29,6 @@ constexpr float kMinValueScale = 0x1p-96f;
 constexpr int64_t kMaxNorm = 512;
 // query rows of one call of several tokens a sequence
 constexpr int64_t kMaxRows = int64_t(1) << 30;
-// channels of a call's sequences that tokens are kept of: 2^25 columns of 16 bytes, 2^21 blocks of 16
-constexpr int64_t kMaxKept = int64_t(1) << 31;
 // caps of scores: the tanh is off by 2e-7, times the cap
 constexpr float kMinCap = 0x1p-10f, kMaxCap = 1024.0f;
 
@@ -458,8 +457,9 @@ quartz_status quartz_paged_keep(const int32_t* first, const int32_t* kept, int64
 {
     if (sequences < 0 || most < 0 || most > kMaxPositions || heads <= 0 || heads > kMaxK ||
         kept_stride < most || kept_stride > kMaxStride || !product_ok(sequences, heads, kMaxBlocks512) ||
-        d <= 0 || d > kMaxK || !product_ok(sequences, heads * d, kMaxKept) || table_pages < 0 ||
-        table_pages > kMaxPositions)
+        d <= 0 || d > kMaxK ||
+        !product_ok(sequences, paged_keep_blocks(heads, d, cache_type == QUARTZ_CACHE_E4M3), kMaxBlocks256) ||
+        table_pages < 0 || table_pages > kMaxPositions)
         return QUARTZ_ERR_SHAPE;
     PagedKeep a{};
     a.cache = {k_cache, v_cache, pages, page_stride, (int32_t)heads, (int32_t)d, shift_of(page_size),

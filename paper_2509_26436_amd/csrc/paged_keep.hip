@@ -80,10 +80,15 @@ __global__ __launch_bounds__(kThreads) void paged_keep_kernel(const PagedKeep a,
 
 }  // namespace
 
+int64_t paged_keep_blocks(int64_t heads, int64_t d, bool fp8)
+{
+    const int64_t pieces = d * (fp8 ? 1 : 2) / 16;
+    return (2 * heads * pieces + kColumns - 1) / kColumns;
+}
+
 hipError_t launch_paged_keep(const PagedKeep& a, hipStream_t stream)
 {
-    const int64_t pieces = a.cache.d * (a.cache.fp8 ? 1 : 2) / 16;
-    const int64_t blocks = (2 * a.cache.heads * pieces + kColumns - 1) / kColumns;
+    const int64_t blocks = paged_keep_blocks(a.cache.heads, a.cache.d, a.cache.fp8);
     paged_keep_kernel<<<(uint32_t)(a.cache.sequences * blocks), kThreads, 0, stream>>>(a, (uint32_t)blocks);
     return hipGetLastError();
 }

@@ -367,6 +367,7 @@ struct PagedKeep {
     const int32_t* kept;
     int64_t kept_stride, most;
 };
+int64_t paged_keep_blocks(int64_t heads, int64_t d, bool fp8);     // of a sequence, 256 threads each
 hipError_t launch_paged_keep(const PagedKeep& a, hipStream_t stream);
 
 // One new token a sequence: o [sequences][heads][d] from q.
