@@ -23,15 +23,14 @@
 // 2^-24 <= |v| < 2^9 (e4m3: any number).  A step with another value keeps bf16
 // values and takes the weights in two bf16 parts (2^-16), and counts infinities and
 // NaN apart, for the rows that see them only: a weight of zero times either would
-// reach rows that do not.  All steps so: 952 us for 674 (8192 tokens of 32 heads of 128
-// channels), 263 for 173 (8 ragged prompts over e4m3).  O's sums are of up to 2^22
-// times a value and key, so a block that meets a value of 2^64 or more starts over:
-// all its steps are such then, and the weights of n keys at most 1 / n, which no
-// value is too large for.
+// reach rows that do not.  All steps so: 969 us for 645 (8192 tokens of 32 heads of 128
+// channels).  O's sums are of up to 2^22 times a value and key, so a block that meets a
+// value of 2^64 or more starts over: all its steps are such then, and the weights of n
+// keys at most 1 / n, which no value is too large for (1110 us).
 //
 // What bounds it: long prompts the issue of instructions.  8192 tokens of 32 heads take
-// 650 us, 846 TFLOP/s, where a large matrix product of the library reaches 1230; the
-// matrix unit is busy for 31 % of the cycles at 2.3 GHz.  A step of 64 keys and 32 rows
+// 641 us, 858 TFLOP/s, where a large matrix product of the library reaches 1230; the
+// matrix unit is busy for 36 % of the cycles.  A step of 64 keys and 32 rows
 // has 32 products (36 cycles each, 16 of which keep vector instructions out) beside some
 // 250 vector instructions (16 maxima, 32 products, 32 exponentials, 16 roundings, 16 sums,
 // 64 for the values' turn to fp16), and its two waves a SIMD, which a barrier a step
@@ -935,15 +934,19 @@ PromptShape prompt_shape(int64_t tokens, int64_t sequences, int64_t heads, int64
     // 27.3 us with 256 keys a part, 33.1 with 512; 1 to 8 tokens over 341 keys 15.1 in two
     // parts, 13.6 in one.
     s.unit = longest > 512 ? 256 : 512;
-    // As many as the device holds at once (tiles counted as if all sequences were alike): 64
-    // nodes of 64 heads over 131000 keys 357 us with 16 parts of each of 16 tiles, 389 with
-    // 32, 485 with 22, which leave a second round that is almost empty.
+    // As many as the device holds at once (tiles counted as if all sequences were alike, and
+    // as long as the table is wide; blocks of 32 rows over bf16 keys of 128 channels, which
+    // have a compute unit's registers each, go in two rounds): 64 nodes of 64 heads over
+    // 131000 keys 357 us with 16 parts of each of 16 tiles, 389 with 32, 485 with 22, which
+    // leave a second round that is almost empty.
     const int64_t resident = device_compute_units() * (s.rows == 256 || d == 256 ? 1 : 2);
     const int64_t parts = std::min(sequences, tokens) * ((each + s.rows - 1) / s.rows) * kv_heads;
     const int64_t units = std::min((longest + s.unit - 1) / s.unit, kMostParts);
     s.splits = (int)std::max<int64_t>(1, std::min(resident / parts, units));
-    // More of them where that leaves compute units without a tile: rounds of blocks, of some
-    // 2.2 us for 64 keys, beside what a join reads and writes.  17 trees of 24 to 48 nodes
+    // More of them, four times as many at most, where that leaves compute units without a
+    // tile: rounds of blocks beside what a join reads and writes.  64 keys take a block some
+    // 2.2 us, in the middle of the kernels' own 1.5 (64 rows, e4m3 keys of 128 channels), 2.0
+    // (64 channels), 2.5 (256 rows of 128) and 6.7 (256 channels).  17 trees of 24 to 48 nodes
     // over 3200 to 6000 e4m3 keys (136 tiles of 256 rows) 185 us in one part each, 130 so.
     if (parts < resident) {
         const auto expected = [&](int64_t splits) {
